@@ -44,7 +44,7 @@ extern "C" {
 #define SQP_ERR_NULL (-1)    /* a required pointer is NULL */
 #define SQP_ERR_SHAPE (-2)   /* a shape rule above is violated */
 #define SQP_ERR_ALIGN (-3)   /* a pointer is not 16-byte aligned */
-#define SQP_ERR_ARG (-4)     /* alpha outside [0, 1] or not finite */
+#define SQP_ERR_ARG (-4)     /* alpha outside [0, 1] or not finite; eps, scale or type out of range */
 #define SQP_ERR_LAUNCH (-5)  /* the HIP runtime reported an error at launch */
 #define SQP_ERR_WORKSPACE (-6) /* the workspace is too small for the launch plan of this shape */
 
@@ -231,6 +231,64 @@ size_t sqp_alpha_search_scratch_bytes(int T, int N, int K, int group, int n_alph
 size_t sqp_alpha_search_scratch_least_bytes(int T, int N, int K, int group, int n_alpha);
 int sqp_alpha_search_scratch(int T, int N, int K, int group, int n_alpha, const float *alphas, const void *x_cal,
                              const void *w, void *scratch, size_t scratch_bytes, double *loss, int *best, void *stream);
+
+/* Element types of a key / value cache and of quantised activations.  SQP_E4M3: 8 bits, 4 of exponent and 3 of mantissa, no
+ * infinities, largest value 448.  An 8-bit row has one fp32 scale: it stands for code * scale, with
+ *   scale = max|row| / 127 (SQP_INT8) or / 448 (SQP_E4M3),  code = round-to-nearest-even(row * (127 or 448) / max|row|);
+ * a row whose largest magnitude is below 2^-100 is stored as zeros with scale 0, one with an infinity or NaN with scale NaN. */
+#define SQP_FP16 0
+#define SQP_INT8 1
+#define SQP_E4M3 2
+
+/* The residual's addition and the RMS norm behind it: sum = fp16(x + residual), y = sqp_rmsnorm(sum) (fp32 arithmetic, one
+ * rounding at the end).  x, residual, sum, y [M][H] fp16, gamma [H] fp16, H % 8 == 0, 0 <= eps < 1.  sum may be x or residual
+ * itself; y may be none of the others. */
+int sqp_add_rmsnorm(int M, int H, const void *x, const void *residual, const void *gamma, float eps, void *y, void *sum, void *stream);
+
+/* The same with y quantised per row (type SQP_INT8 or SQP_E4M3) before any rounding to fp16: codes [M][H], scales [M] fp32. */
+int sqp_add_rmsnorm_quant(int M, int H, int type, const void *x, const void *residual, const void *gamma, float eps, void *codes,
+                          float *scales, void *sum, void *stream);
+
+/* Paged cache of keys and values, D = 64 or 128 values per token and head, `page` tokens per page (a power of two from 16 to 65536):
+ *   k_cache, v_cache    [pages][kv_heads][page][D] of `type`; pages * page < 2^31, the tensors may have more elements than that
+ *   k_scales, v_scales  [pages][kv_heads][page] fp32 (8-bit types; NULL for SQP_FP16)
+ * A slot is a token's place: page number * page + place in the page.  Index arrays (slots, positions, page tables, lengths,
+ * starts) are int32 and need 4-byte alignment only.
+ *
+ * Writes the keys and values of T tokens into their slots; on the way keys, and queries if there are any, are rotated:
+ *   y[j] = x[j] c[j] - x[D/2 + j] s[j],  y[D/2 + j] = x[D/2 + j] c[j] + x[j] s[j],  c | s = cos_sin[position], fp32
+ * (cos_sin [n_positions][D] fp32: D/2 cosines, D/2 sines; NULL: no rotation), and keys and values are quantised from these
+ * fp32 values.  q [T][heads][D], k, v [T][kv_heads][D] fp16 with the given distances between tokens (elements, multiples of 8),
+ * q_out [T][heads][D] fp16 (heads == 0: no queries, q and q_out unused).  A token whose slot lies outside the cache (-1, say)
+ * is not written; one whose position lies outside the table becomes NaN.  Two tokens in one slot: either may end there.
+ * T == 0 enqueues nothing. */
+int sqp_kv_cache_write(int T, int heads, int kv_heads, int D, int type, int page, int pages, const void *q, long q_stride, const void *k,
+                       long k_stride, const void *v, long v_stride, const int *slots, const float *cos_sin, const int *positions,
+                       int n_positions, void *k_cache, void *v_cache, float *k_scales, float *v_scales, void *q_out, void *stream);
+
+/* Reads T slots back: k, v [T][kv_heads][D] fp16 = fp16(code * scale); zeros for a slot outside the cache. */
+int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages, const int *slots, const void *k_cache, const void *v_cache,
+                      const float *k_scales, const float *v_scales, void *k, void *v, void *stream);
+
+/* Attention of the newest tokens of B sequences over the paged cache, which holds these tokens' keys and values already:
+ *   out[t][h] = sum_j p_j v_j,  p = softmax_j (scale q[t][h] . k_j),  h reading the cached head h / (heads / kv_heads)
+ * Sequence b has seq_lens[b] cached tokens, token j in page page_table[b][j / page]; its new tokens are the rows
+ * q_starts[b] .. q_starts[b + 1] - 1 of q (q_starts [B + 1], not decreasing; NULL: T == B, one token each).  The i-th of its n
+ * new tokens sees the tokens j <= seq_lens[b] - n + i.  A token that sees nothing, or belongs to no sequence, gets zeros.
+ *   q [T][heads][D] fp16, q_stride elements between tokens; out [T][heads][D] fp16
+ *   page_table [B][table_width] int32, table_stride entries between rows; entries past a sequence's length are not read
+ *   max_q, max_len  the most new tokens and the greatest length of a sequence, as far as the caller knows: the work is laid
+ *                   out by them.  Larger ones in the arrays are computed as well, only slower.  0: not known.
+ *   scratch         of this call alone until its work has run, sqp_paged_attention_scratch_bytes() for the preferred plan;
+ *                   smaller or NULL: a plan that fits
+ * Scores, softmax and sums are fp32; p is rounded to fp16 for the matrix cores (relative 2^-11).  What lies past a sequence's length is not
+ * used, whatever it holds; nor does a token that sees less depend on the later ones, be they infinite or NaN.  Page numbers outside the cache,
+ * lengths past the table and starts past T are taken as the nearest that is inside.  Deterministic.  B <= 65535. */
+size_t sqp_paged_attention_scratch_bytes(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len);
+int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D, int type, int page, int pages, int table_width, int max_q, int max_len,
+                        float scale, const void *q, long q_stride, const void *k_cache, const void *v_cache, const float *k_scales,
+                        const float *v_scales, const int *page_table, long table_stride, const int *seq_lens, const int *q_starts, void *out,
+                        void *scratch, size_t scratch_bytes, void *stream);
 
 #pragma GCC visibility pop
 #ifdef __cplusplus

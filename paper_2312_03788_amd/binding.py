@@ -17,7 +17,8 @@ _LIB_PATH = os.environ.get("SQP_LIBRARY", os.path.join(_HERE, "libsqp.so"))  # o
 EXPORTS = ["sqp_status_string", "sqp_smooth_scales", "sqp_smooth_apply_x", "sqp_smooth_apply_w",
            "sqp_quantize_pack", "sqp_dequantize", "sqp_w4a16_gemm", "sqp_quant_loss", "sqp_transpose_nk",
            "sqp_w4a16_gemm_silu_mul", "sqp_rmsnorm", "sqp_scale_columns", "sqp_interleave_gate_up",
-           "sqp_set_workspace", "sqp_alpha_search", "sqp_w4a16_gemm_static", "sqp_w4a16_gemm_scratch", "sqp_alpha_search_scratch"]
+           "sqp_set_workspace", "sqp_alpha_search", "sqp_w4a16_gemm_static", "sqp_w4a16_gemm_scratch", "sqp_alpha_search_scratch",
+           "sqp_add_rmsnorm", "sqp_add_rmsnorm_quant", "sqp_kv_cache_write", "sqp_kv_cache_read", "sqp_paged_attention"]
 
 
 class SqpError(RuntimeError):
@@ -66,6 +67,14 @@ def lib():
         L.sqp_w4a16_gemm_workspace_bytes.restype = ctypes.c_size_t
         L.sqp_w4a16_gemm_workspace_least_bytes.argtypes = [i, i, i, i]
         L.sqp_w4a16_gemm_workspace_least_bytes.restype = ctypes.c_size_t
+        ll, sz = ctypes.c_long, ctypes.c_size_t
+        L.sqp_add_rmsnorm.argtypes = [i, i, vp, vp, vp, f, vp, vp, vp]
+        L.sqp_add_rmsnorm_quant.argtypes = [i, i, i, vp, vp, vp, f, vp, vp, vp, vp]
+        L.sqp_kv_cache_write.argtypes = [i] * 7 + [vp, ll, vp, ll, vp, ll, vp, vp, vp, i, vp, vp, vp, vp, vp, vp]
+        L.sqp_kv_cache_read.argtypes = [i] * 6 + [vp] * 8
+        L.sqp_paged_attention.argtypes = [i] * 11 + [f, vp, ll, vp, vp, vp, vp, vp, ll, vp, vp, vp, vp, sz, vp]
+        L.sqp_paged_attention_scratch_bytes.argtypes = [i] * 7
+        L.sqp_paged_attention_scratch_bytes.restype = sz
         for name in EXPORTS[1:]:
             getattr(L, name).restype = ctypes.c_int
         L.sqp_quant_loss_scratch_doubles.restype = ctypes.c_long
@@ -78,6 +87,9 @@ def lib():
         fast.bind_preparation(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.sqp_smooth_apply_w, L.sqp_scale_columns, L.sqp_smooth_scales, L.sqp_quantize_pack, L.sqp_dequantize,
             L.sqp_transpose_nk, L.sqp_interleave_gate_up)])
+        fast.bind_layer(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.sqp_add_rmsnorm, L.sqp_add_rmsnorm_quant, L.sqp_kv_cache_write, L.sqp_kv_cache_read, L.sqp_paged_attention,
+            L.sqp_paged_attention_scratch_bytes)])
         _fast = fast
         _lib = L
     return _lib
@@ -432,3 +444,194 @@ def alpha_search(x_cal, w, group=128, alphas=None):
     vals = [float(v) for v in loss.cpu()]
     b = int(best.cpu()[0])
     return float(alphas[b]), list(zip([float(a) for a in alphas], vals))
+
+
+# ---------------------------------------------------------------- between the linears: residual and norm, cache, attention
+
+_TYPES = {torch.float16: 0, torch.int8: 1, torch.float8_e4m3fn: 2}  # SQP_FP16, SQP_INT8, SQP_E4M3
+
+
+def add_rmsnorm(x, residual, gamma, eps, out=None, sum_out=None):
+    """(y, r): the new residual r = x + residual and its RMS norm y, both fp16 [M,H].  sum_out may be x or residual."""
+    if _native(x):
+        o = _fast.add_rmsnorm(0, x, residual, gamma, eps, out, sum_out, *_here())
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_add_rmsnorm")
+    M, H = x.shape
+    _shaped(residual, (M, H), "residual")
+    _shaped(gamma, (H,), "gamma")
+    y = out if out is not None else torch.empty_like(x)
+    r = sum_out if sum_out is not None else torch.empty_like(x)
+    _shaped(y, (M, H), "out")
+    _shaped(r, (M, H), "sum_out")
+    _check(lib().sqp_add_rmsnorm(M, H, _dev(x, torch.float16, "x"), _dev(residual, torch.float16, "residual"), _dev(gamma, torch.float16, "gamma"),
+                                 float(eps), _dev(y, torch.float16, "out"), _dev(r, torch.float16, "sum_out"), _stream()), "sqp_add_rmsnorm")
+    return y, r
+
+
+def add_rmsnorm_quant(x, residual, gamma, eps, dtype=torch.float8_e4m3fn, out=None, sum_out=None):
+    """(codes, scales, r): add_rmsnorm with y in 8 bits (torch.int8 or torch.float8_e4m3fn [M,H]) and an fp32 scale per
+    row [M].  out: (codes, scales)."""
+    kind = _TYPES.get(dtype, 0)
+    if kind and out is None and _native(x):
+        o = _fast.add_rmsnorm(kind, x, residual, gamma, eps, None, sum_out, *_here())
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_add_rmsnorm_quant")
+    if not kind:
+        raise SqpError("dtype must be torch.int8 or torch.float8_e4m3fn")
+    M, H = x.shape
+    _shaped(residual, (M, H), "residual")
+    _shaped(gamma, (H,), "gamma")
+    codes, scales = out if out is not None else (torch.empty((M, H), dtype=dtype, device=x.device),
+                                                 torch.empty(M, dtype=torch.float32, device=x.device))
+    r = sum_out if sum_out is not None else torch.empty_like(x)
+    _shaped(codes, (M, H), "codes")
+    _shaped(scales, (M,), "scales")
+    _shaped(r, (M, H), "sum_out")
+    _check(lib().sqp_add_rmsnorm_quant(M, H, kind, _dev(x, torch.float16, "x"), _dev(residual, torch.float16, "residual"),
+                                       _dev(gamma, torch.float16, "gamma"), float(eps), _dev(codes, dtype, "codes"),
+                                       _dev(scales, torch.float32, "scales"), _dev(r, torch.float16, "sum_out"), _stream()), "sqp_add_rmsnorm_quant")
+    return codes, scales, r
+
+
+def _shaped(t, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise SqpError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+
+
+def _heads(t, name):
+    """Pointer of a tensor [T, heads, D] fp16 whose tokens may lie apart (a view of a merged projection)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise SqpError("%s must be a GPU tensor" % name)
+    if t.dtype != torch.float16:
+        raise SqpError("%s must have dtype torch.float16, got %s" % (name, t.dtype))
+    if t.dim() != 3 or (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
+        raise SqpError("%s must be [tokens, heads, D] with the values of a token contiguous" % name)
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _step(t):
+    """Distance between tokens of [T, heads, D]."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _cache(k_cache, v_cache, k_scales, v_scales):
+    """Arguments of a cache: (pages, kv_heads, page, D, type) and its four pointers."""
+    if k_cache.dim() != 4 or k_cache.dtype not in _TYPES:
+        raise SqpError("k_cache must be [pages, kv_heads, page, D] of torch.float16, torch.int8 or torch.float8_e4m3fn")
+    _shaped(v_cache, k_cache.shape, "v_cache")
+    ptrs = [_dev(k_cache, k_cache.dtype, "k_cache"), _dev(v_cache, k_cache.dtype, "v_cache"), None, None]
+    kind = _TYPES[k_cache.dtype]
+    if kind:
+        for at, (s, name) in enumerate(((k_scales, "k_scales"), (v_scales, "v_scales"))):
+            if s is None:
+                raise SqpError("an 8-bit cache needs %s" % name)
+            _shaped(s, k_cache.shape[:3], name)
+            ptrs[2 + at] = _dev(s, torch.float32, name)
+    elif k_scales is not None or v_scales is not None:
+        raise SqpError("an fp16 cache has no scales")
+    return tuple(k_cache.shape) + (kind,), ptrs
+
+
+def kv_cache_write(k, v, slots, k_cache, v_cache, k_scales=None, v_scales=None, q=None, cos_sin=None, positions=None, out=None):
+    """Keys and values [T, kv_heads, D] of T tokens into their slots (page * tokens per page + place; int32 [T], outside the
+    cache: not written) of the cache [pages, kv_heads, page, D] (fp16, or int8 / e4m3 with scales [pages, kv_heads, page]).
+    With cos_sin [positions, D] fp32 and positions int32 [T], keys and q are rotated; returns the queries [T, heads, D], or None
+    without q.  q, k and v may be views of a merged projection."""
+    if _native(k):
+        o = _fast.kv_cache_write(k, v, slots, k_cache, v_cache, k_scales, v_scales, q, cos_sin, positions, out, *_here())
+        if o is not None:
+            return (None if o is True else o) if type(o) is not int else _ended(o, "sqp_kv_cache_write")
+    (pages, kv_heads, page, D, kind), cache = _cache(k_cache, v_cache, k_scales, v_scales)
+    kp, vp = _heads(k, "k"), _heads(v, "v")
+    T = k.shape[0]
+    _shaped(k, (T, kv_heads, D), "k")
+    _shaped(v, (T, kv_heads, D), "v")
+    _shaped(slots, (T,), "slots")
+    heads, qp, op, q_step = 0, None, None, 0
+    if q is not None:
+        qp, heads, q_step = _heads(q, "q"), q.shape[1], _step(q)
+        _shaped(q, (T, heads, D), "q")
+        out = out if out is not None else torch.empty((T, heads, D), dtype=torch.float16, device=q.device)
+        _shaped(out, (T, heads, D), "out")
+        op = _dev(out, torch.float16, "out")
+    cs, ps, n_positions = None, None, 0
+    if cos_sin is not None:
+        if positions is None:
+            raise SqpError("cos_sin needs positions")
+        n_positions = cos_sin.shape[0]
+        _shaped(cos_sin, (n_positions, D), "cos_sin")
+        _shaped(positions, (T,), "positions")
+        cs, ps = _dev(cos_sin, torch.float32, "cos_sin"), _dev(positions, torch.int32, "positions")
+    if T > 0:
+        _check(lib().sqp_kv_cache_write(T, heads, kv_heads, D, kind, page, pages, qp, q_step, kp, _step(k), vp, _step(v), _dev(slots, torch.int32, "slots"),
+                                        cs, ps, n_positions, *cache, op, _stream()), "sqp_kv_cache_write")
+    return out if q is not None else None
+
+
+def kv_cache_read(slots, k_cache, v_cache, k_scales=None, v_scales=None, out=None):
+    """(k, v): the slots' keys and values as fp16 [T, kv_heads, D] (zeros for slots outside the cache).  out: (k, v)."""
+    if out is None and _native(slots):
+        o = _fast.kv_cache_read(slots, k_cache, v_cache, k_scales, v_scales, *_here())
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_kv_cache_read")
+    (pages, kv_heads, page, D, kind), cache = _cache(k_cache, v_cache, k_scales, v_scales)
+    if slots.dim() != 1:
+        raise SqpError("slots must have one dimension")
+    T = slots.shape[0]
+    k, v = out if out is not None else [torch.empty((T, kv_heads, D), dtype=torch.float16, device=slots.device) for _ in range(2)]
+    _shaped(k, (T, kv_heads, D), "k")
+    _shaped(v, (T, kv_heads, D), "v")
+    sp = _dev(slots, torch.int32, "slots")
+    if T > 0:
+        _check(lib().sqp_kv_cache_read(T, kv_heads, D, kind, page, pages, sp, *cache, _dev(k, torch.float16, "k"), _dev(v, torch.float16, "v"),
+                                       _stream()), "sqp_kv_cache_read")
+    return k, v
+
+
+def paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts=None, k_scales=None, v_scales=None, max_q=None, max_len=None,
+                    scale=None, out=None):
+    """Attention of the newest tokens of B sequences (q [T, heads, D] fp16) over the paged cache, which holds their keys and
+    values already: fp16 [T, heads, D].  page_table int32 [B, pages of a sequence], seq_lens int32 [B] (cached tokens, the new
+    ones among them), q_starts int32 [B + 1] (None: one new token per sequence).  max_q, max_len: the most new tokens and the
+    greatest length, if the caller knows them (the work is laid out by them; larger ones are right, only slower).  scale: of the
+    scores, D^-0.5 by default."""
+    if _native(q):
+        o = _fast.paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts, k_scales, v_scales, max_q, max_len, scale, out, *_here())
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_paged_attention")
+    (pages, kv_heads, page, D, kind), cache = _cache(k_cache, v_cache, k_scales, v_scales)
+    qp = _heads(q, "q")
+    T, heads = q.shape[:2]
+    _shaped(q, (T, heads, D), "q")
+    if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise SqpError("page_table must be [sequences, pages] with contiguous rows")
+    B, width = page_table.shape
+    _shaped(seq_lens, (B,), "seq_lens")
+    table = _dev(page_table[:1] if B > 1 else page_table, torch.int32, "page_table")
+    lens = _dev(seq_lens, torch.int32, "seq_lens")
+    starts = None
+    if q_starts is not None:
+        _shaped(q_starts, (B + 1,), "q_starts")
+        starts = _dev(q_starts, torch.int32, "q_starts")
+    elif T != B:
+        raise SqpError("without q_starts q has one token per sequence")
+    if heads % kv_heads:
+        raise SqpError("heads must be a multiple of kv_heads")
+    o = out if out is not None else torch.empty((T, heads, D), dtype=torch.float16, device=q.device)
+    _shaped(o, (T, heads, D), "out")
+    op = _dev(o, torch.float16, "out")
+    max_q, max_len = int(max_q or 0), int(max_len or 0)
+    scratch, nbytes = None, 0
+    if T > 0 and not (out is not None and torch.cuda.is_current_stream_capturing()):
+        nbytes = int(lib().sqp_paged_attention_scratch_bytes(T, B, heads, kv_heads, D, max_q, max_len or width * page))
+        if nbytes:
+            try:
+                scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+            except torch.cuda.OutOfMemoryError:
+                nbytes = 0
+    if T > 0:
+        _check(lib().sqp_paged_attention(T, B, heads, kv_heads, D, kind, page, pages, width, max_q, max_len, float(D ** -0.5 if scale is None else scale),
+                                         qp, _step(q), *cache, table, page_table.stride(0) if B > 1 else width, lens, starts, op,
+                                         ctypes.c_void_p(scratch.data_ptr()) if scratch is not None else None, nbytes, _stream()), "sqp_paged_attention")
+    return o

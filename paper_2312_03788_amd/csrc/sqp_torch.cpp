@@ -1,4 +1,4 @@
-// Argument marshalling of the serving calls (GEMM, RMSNorm, activation smoothing) and of the calls that
+// Argument marshalling of the serving calls (GEMM, norms, activation smoothing, cache, attention) and of the calls that
 // prepare a weight for torch tensors, in C++: a decode launch takes 5 to 15 us on the GPU, the same checks and
 // the ctypes conversion in Python 11 us per GEMM call; the calls on a 1024 x 1024 weight take 9 to 14 us of
 // host time in Python and 4 to 7 here.  Holds no arithmetic and no state but the addresses of the
@@ -38,6 +38,15 @@ typedef int (*UnpackFn)(int, int, int, const uint32_t *, const void *, const uin
 typedef int (*TransposeFn)(int, int, const void *, void *, void *);
 typedef int (*InterleaveFn)(int, int, const void *, const void *, void *, void *);
 
+typedef int (*AddNormFn)(int, int, const void *, const void *, const void *, float, void *, void *, void *);
+typedef int (*AddNormQuantFn)(int, int, int, const void *, const void *, const void *, float, void *, float *, void *, void *);
+typedef int (*CacheWriteFn)(int, int, int, int, int, int, int, const void *, long, const void *, long, const void *, long, const int *, const float *,
+                            const int *, int, void *, void *, float *, float *, void *, void *);
+typedef int (*CacheReadFn)(int, int, int, int, int, int, const int *, const void *, const void *, const float *, const float *, void *, void *, void *);
+typedef int (*AttentionFn)(int, int, int, int, int, int, int, int, int, int, int, float, const void *, long, const void *, const void *, const float *,
+                           const float *, const int *, long, const int *, const int *, void *, void *, size_t, void *);
+typedef size_t (*AttentionScratchFn)(int, int, int, int, int, int, int);
+
 GemmFn g_gemm[3];  // plain, fused activation, static scratch
 WorkspaceFn g_workspace_bytes, g_scratch_bytes;
 ScratchGemmFn g_gemm_scratch;
@@ -48,6 +57,12 @@ PackFn g_pack;
 UnpackFn g_unpack;
 TransposeFn g_transpose;
 InterleaveFn g_interleave;
+AddNormFn g_add_norm;
+AddNormQuantFn g_add_norm_quant;
+CacheWriteFn g_cache_write;
+CacheReadFn g_cache_read;
+AttentionFn g_attention;
+AttentionScratchFn g_attention_scratch;
 
 // The tensor behind an argument if it is a dense GPU tensor of this type on device `dev`, else null.  A
 // subclass other than torch.nn.Parameter has semantics of its own (__torch_function__, the type of
@@ -389,7 +404,259 @@ PyObject *bind_preparation(PyObject *, PyObject *const *a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// add_rmsnorm(type, x, residual, gamma, eps, out, sum out, device, stream): new (y, sum) or (codes, scales, sum)
+PyObject *add_rmsnorm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 9 || !g_add_norm || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    const long type = PyLong_AsLong(a[0]);
+    const double eps = PyFloat_AsDouble(a[4]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    if (type < 0 || type > 2 || (type && a[5] != Py_None)) Py_RETURN_NONE;
+    try {
+        const at::Tensor *x = plain(a[1], at::kHalf, dev), *residual = plain(a[2], at::kHalf, dev), *gamma = plain(a[3], at::kHalf, dev);
+        if (!x || !residual || !gamma || x->dim() != 2 || !residual->sizes().equals(x->sizes()) || gamma->dim() != 1 || gamma->size(0) != x->size(1)) Py_RETURN_NONE;
+        const long M = x->size(0), H = x->size(1);
+        if (!fits(M) || !fits(H)) Py_RETURN_NONE;
+        at::Tensor y, sum, scales;
+        for (int i = 5; i < 7; i++) {  // (given outputs have the shape of x)
+            const at::Tensor *t = a[i] == Py_None ? x : plain(a[i], at::kHalf, dev);
+            if (!t || !t->sizes().equals(x->sizes())) Py_RETURN_NONE;
+            (i == 5 ? y : sum) = a[i] == Py_None ? fresh({M, H}, i == 6 || type == 0 ? at::kHalf : type == 1 ? at::kChar : at::kFloat8_e4m3fn, *x) : *t;
+        }
+        if (type) scales = fresh({M}, at::kFloat, *x);
+        const void *xp = x->data_ptr(), *rp = residual->data_ptr(), *gp = gamma->data_ptr();
+        void *yp = y.data_ptr(), *sp = sum.data_ptr(), *cp = type ? scales.data_ptr() : nullptr;
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        if (type) rc = g_add_norm_quant((int)M, (int)H, (int)type, xp, rp, gp, (float)eps, yp, (float *)cp, sp, stream);
+        else rc = g_add_norm((int)M, (int)H, xp, rp, gp, (float)eps, yp, sp, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != 0) return PyLong_FromLong(rc);
+        PyObject *yo = a[5], *so = a[6];
+        if (yo == Py_None) yo = THPVariable_Wrap(y);
+        else Py_INCREF(yo);
+        if (so == Py_None) so = THPVariable_Wrap(sum);
+        else Py_INCREF(so);
+        return type ? Py_BuildValue("(NNN)", yo, THPVariable_Wrap(scales), so) : Py_BuildValue("(NN)", yo, so);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// A tensor [tokens, heads, D] in fp16 whose tokens may lie apart, and the distance between them; else null.
+const at::Tensor *tokens(PyObject *o, long dev, long &step)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || t.key_set().has(c10::DispatchKey::Python) || t.layout() != at::kStrided || !t.is_cuda()) return nullptr;
+    if (t.scalar_type() != at::kHalf || t.get_device() != dev || t.dim() != 3 || t.size(0) <= 0 || t.size(0) > INT_MAX) return nullptr;
+    if (t.stride(2) != 1 || (t.size(1) > 1 && t.stride(1) != t.size(2))) return nullptr;
+    step = t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
+    return &t;
+}
+
+struct Cache {
+    const at::Tensor *k, *v, *k_scales, *v_scales;
+    int pages, kv_heads, page, D, type;
+    void *kp, *vp;
+    float *ksp, *vsp;
+};
+
+// The cache of four arguments: k_cache, v_cache, k_scales, v_scales.
+bool cache(PyObject *const *a, long dev, Cache &c)
+{
+    if (!THPVariable_CheckExact(a[0])) return false;
+    const at::Tensor &t = THPVariable_Unpack(a[0]);
+    if (!t.defined()) return false;
+    const at::ScalarType type = t.scalar_type();
+    c.type = type == at::kHalf ? 0 : type == at::kChar ? 1 : type == at::kFloat8_e4m3fn ? 2 : -1;
+    if (c.type < 0) return false;
+    c.k = plain(a[0], type, dev);
+    c.v = plain(a[1], type, dev);
+    if (!c.k || !c.v || c.k->dim() != 4 || !c.v->sizes().equals(c.k->sizes())) return false;
+    for (int i = 0; i < 4; i++)
+        if (!fits(c.k->size(i))) return false;
+    c.pages = (int)c.k->size(0); c.kv_heads = (int)c.k->size(1); c.page = (int)c.k->size(2); c.D = (int)c.k->size(3);
+    c.kp = c.k->data_ptr();
+    c.vp = c.v->data_ptr();
+    c.ksp = c.vsp = nullptr;
+    if (c.type == 0) return a[2] == Py_None && a[3] == Py_None;
+    c.k_scales = plain(a[2], at::kFloat, dev);
+    c.v_scales = plain(a[3], at::kFloat, dev);
+    if (!c.k_scales || !c.v_scales) return false;
+    if (!c.k_scales->sizes().equals(c.k->sizes().slice(0, 3)) || !c.v_scales->sizes().equals(c.k->sizes().slice(0, 3))) return false;
+    c.ksp = (float *)c.k_scales->data_ptr();
+    c.vsp = (float *)c.v_scales->data_ptr();
+    return true;
+}
+
+bool is_tokens(const at::Tensor *t, long T, long heads, long D) { return t && t->size(0) == T && t->size(1) == heads && t->size(2) == D; }
+
+// kv_cache_write(k, v, slots, k_cache, v_cache, k_scales, v_scales, q, cos_sin, positions, out, device, stream): the queries, or
+// True where there are none
+PyObject *kv_cache_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 13 || !g_cache_write || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    try {
+        Cache c;
+        if (!cache(a + 3, dev, c)) Py_RETURN_NONE;
+        long k_step, v_step, q_step = 0;
+        const at::Tensor *k = tokens(a[0], dev, k_step), *v = tokens(a[1], dev, v_step), *slots = plain(a[2], at::kInt, dev);
+        if (!k || !is_tokens(k, k->size(0), c.kv_heads, c.D) || !is_tokens(v, k->size(0), c.kv_heads, c.D)) Py_RETURN_NONE;
+        const long T = k->size(0);
+        if (!slots || slots->dim() != 1 || slots->size(0) != T) Py_RETURN_NONE;
+        const at::Tensor *q = nullptr, *cos_sin = nullptr, *positions = nullptr;
+        at::Tensor y;
+        if (a[7] != Py_None) {
+            q = tokens(a[7], dev, q_step);
+            if (!q || !is_tokens(q, T, q->size(1), c.D) || !fits(q->size(1))) Py_RETURN_NONE;
+            if (a[10] == Py_None) {
+                y = fresh({T, q->size(1), c.D}, at::kHalf, *q);
+            } else {
+                const at::Tensor *o = plain(a[10], at::kHalf, dev);
+                if (!o || !o->sizes().equals(q->sizes())) Py_RETURN_NONE;
+                y = *o;
+            }
+        }
+        if (a[8] != Py_None) {
+            cos_sin = plain(a[8], at::kFloat, dev);
+            positions = plain(a[9], at::kInt, dev);
+            if (!cos_sin || cos_sin->dim() != 2 || cos_sin->size(1) != c.D || !fits(cos_sin->size(0))) Py_RETURN_NONE;
+            if (!positions || positions->dim() != 1 || positions->size(0) != T) Py_RETURN_NONE;
+        }
+        const void *qp = q ? q->data_ptr() : nullptr, *kp = k->data_ptr(), *vp = v->data_ptr();
+        const int *sp = (const int *)slots->data_ptr(), *pp = positions ? (const int *)positions->data_ptr() : nullptr;
+        const float *cp = cos_sin ? (const float *)cos_sin->data_ptr() : nullptr;
+        const int heads = q ? (int)q->size(1) : 0, n_positions = cos_sin ? (int)cos_sin->size(0) : 0;
+        void *yp = q ? y.data_ptr() : nullptr;
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_cache_write((int)T, heads, c.kv_heads, c.D, c.type, c.page, c.pages, qp, q_step, kp, k_step, vp, v_step, sp, cp, pp, n_positions, c.kp, c.vp,
+                           c.ksp, c.vsp, yp, stream);
+        Py_END_ALLOW_THREADS
+        if (rc == 0 && !q) Py_RETURN_TRUE;
+        return result(rc, q ? a[10] : Py_None, y);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// kv_cache_read(slots, k_cache, v_cache, k_scales, v_scales, device, stream): new (k, v)
+PyObject *kv_cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 7 || !g_cache_read || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    try {
+        Cache c;
+        const at::Tensor *slots = plain(a[0], at::kInt, dev);
+        if (!slots || slots->dim() != 1 || !fits(slots->size(0)) || !cache(a + 1, dev, c)) Py_RETURN_NONE;
+        const long T = slots->size(0);
+        const at::Tensor k = fresh({T, c.kv_heads, c.D}, at::kHalf, *slots), v = fresh({T, c.kv_heads, c.D}, at::kHalf, *slots);
+        const int *sp = (const int *)slots->data_ptr();
+        void *kp = k.data_ptr(), *vp = v.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_cache_read((int)T, c.kv_heads, c.D, c.type, c.page, c.pages, sp, c.kp, c.vp, c.ksp, c.vsp, kp, vp, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != 0) return PyLong_FromLong(rc);
+        return Py_BuildValue("(NN)", THPVariable_Wrap(k), THPVariable_Wrap(v));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts, k_scales, v_scales, max_q, max_len, scale, out, device, stream)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 14 || !g_attention || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    const long max_q = a[8] == Py_None ? 0 : PyLong_AsLong(a[8]), max_len = a[9] == Py_None ? 0 : PyLong_AsLong(a[9]);
+    const double given = a[10] == Py_None ? 0.0 : PyFloat_AsDouble(a[10]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    if (max_q < 0 || max_q > INT_MAX || max_len < 0 || max_len > INT_MAX) Py_RETURN_NONE;
+    try {
+        Cache c;
+        PyObject *const four[4] = {a[1], a[2], a[6], a[7]};
+        if (!cache(four, dev, c)) Py_RETURN_NONE;
+        long q_step;
+        const at::Tensor *q = tokens(a[0], dev, q_step), *lens = plain(a[4], at::kInt, dev), *starts = nullptr;
+        if (!q || q->size(2) != c.D || !fits(q->size(1)) || q->size(1) % c.kv_heads || !lens || lens->dim() != 1 || !THPVariable_CheckExact(a[3])) Py_RETURN_NONE;
+        const at::Tensor &table = THPVariable_Unpack(a[3]);
+        if (!table.defined() || table.key_set().has(c10::DispatchKey::Python) || table.layout() != at::kStrided || !table.is_cuda()) Py_RETURN_NONE;
+        if (table.scalar_type() != at::kInt || table.get_device() != dev || table.dim() != 2) Py_RETURN_NONE;
+        const long T = q->size(0), heads = q->size(1), B = table.size(0), width = table.size(1);
+        if (!fits(B) || !fits(width) || lens->size(0) != B || (width > 1 && table.stride(1) != 1)) Py_RETURN_NONE;
+        if (a[5] != Py_None) {
+            starts = plain(a[5], at::kInt, dev);
+            if (!starts || starts->dim() != 1 || starts->size(0) != B + 1) Py_RETURN_NONE;
+        } else if (T != B) {
+            Py_RETURN_NONE;
+        }
+        const long reach = width * c.page;
+        const size_t bytes = g_attention_scratch((int)T, (int)B, (int)heads, c.kv_heads, c.D, (int)max_q, (int)(max_len ? max_len : reach > INT_MAX ? INT_MAX : reach));
+        if (bytes > 0 && a[11] != Py_None) Py_RETURN_NONE;  // (the general path looks whether the caller may not allocate)
+        at::Tensor y, scratch;
+        if (a[11] == Py_None) {
+            y = fresh({T, heads, c.D}, at::kHalf, *q);
+        } else {
+            const at::Tensor *o = plain(a[11], at::kHalf, dev);
+            if (!o || !o->sizes().equals(q->sizes())) Py_RETURN_NONE;
+            y = *o;
+        }
+        if (bytes > 0) scratch = fresh({(long)bytes}, at::kByte, *q);  // (dropped on return: whatever takes it next is ordered behind the kernels)
+        const void *qp = q->data_ptr();
+        const int *tp = (const int *)table.data_ptr(), *lp = (const int *)lens->data_ptr(), *sp = starts ? (const int *)starts->data_ptr() : nullptr;
+        const long t_step = B > 1 ? table.stride(0) : width;
+        void *yp = y.data_ptr(), *wp = bytes > 0 ? scratch.data_ptr() : nullptr;
+        const float scale = a[10] == Py_None ? (c.D == 128 ? 0.08838834764831845f : 0.125f) : (float)given;
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_attention((int)T, (int)B, (int)heads, c.kv_heads, c.D, c.type, c.page, c.pages, (int)width, (int)max_q, (int)max_len, scale, qp, q_step, c.kp,
+                         c.vp, c.ksp, c.vsp, tp, t_step, lp, sp, yp, wp, bytes, stream);
+        Py_END_ALLOW_THREADS
+        return result(rc, a[11], y);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// bind_layer(addresses of sqp_add_rmsnorm, _quant, sqp_kv_cache_write, _read, sqp_paged_attention, _scratch_bytes)
+PyObject *bind_layer(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    void *p[6];
+    if (n != 6) {
+        PyErr_SetString(PyExc_TypeError, "bind_layer takes six addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 6; i++) p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+    g_add_norm = (AddNormFn)p[0];
+    g_add_norm_quant = (AddNormQuantFn)p[1];
+    g_cache_write = (CacheWriteFn)p[2];
+    g_cache_read = (CacheReadFn)p[3];
+    g_attention = (AttentionFn)p[4];
+    g_attention_scratch = (AttentionScratchFn)p[5];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
+    {"bind_layer", (PyCFunction)(void (*)(void))bind_layer, METH_FASTCALL, nullptr},
+    {"add_rmsnorm", (PyCFunction)(void (*)(void))add_rmsnorm, METH_FASTCALL, nullptr},
+    {"kv_cache_write", (PyCFunction)(void (*)(void))kv_cache_write, METH_FASTCALL, nullptr},
+    {"kv_cache_read", (PyCFunction)(void (*)(void))kv_cache_read, METH_FASTCALL, nullptr},
+    {"paged_attention", (PyCFunction)(void (*)(void))paged_attention, METH_FASTCALL, nullptr},
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
     {"gemm", (PyCFunction)(void (*)(void))gemm, METH_FASTCALL, nullptr},
     {"rmsnorm", (PyCFunction)(void (*)(void))rmsnorm, METH_FASTCALL, nullptr},
