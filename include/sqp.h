@@ -278,7 +278,8 @@ int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages,
  *   q [T][heads][D] fp16, q_stride elements between tokens; out [T][heads][D] fp16
  *   page_table [B][table_width] int32, table_stride entries between rows; entries past a sequence's length are not read
  *   max_q, max_len  the most new tokens and the greatest length of a sequence, as far as the caller knows: the work is laid
- *                   out by them.  Larger ones in the arrays are computed as well, only slower.  0: not known.
+ *                   out by them.  Larger ones in the arrays are computed as well, only slower.  0: not known
+ *                   (scratch_bytes: max_len = table_width * page then; max_q = 1 without q_starts).
  *   scratch         of this call alone until its work has run, sqp_paged_attention_scratch_bytes() for the preferred plan;
  *                   smaller or NULL: a plan that fits
  * Scores, softmax and sums are fp32; p is rounded to fp16 for the matrix cores (relative 2^-11).  What lies past a sequence's length is not

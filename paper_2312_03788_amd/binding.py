@@ -621,7 +621,7 @@ def paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts=None, k_
     o = out if out is not None else torch.empty((T, heads, D), dtype=torch.float16, device=q.device)
     _shaped(o, (T, heads, D), "out")
     op = _dev(o, torch.float16, "out")
-    max_q, max_len = int(max_q or 0), int(max_len or 0)
+    max_q, max_len = int(max_q or 0) if q_starts is not None else 1, int(max_len or 0)
     scratch, nbytes = None, 0
     if T > 0 and not (out is not None and torch.cuda.is_current_stream_capturing()):
         nbytes = int(lib().sqp_paged_attention_scratch_bytes(T, B, heads, kv_heads, D, max_q, max_len or width * page))

@@ -19,10 +19,71 @@ struct SqpAttention {
     float scale2;  // scale log2(e): the softmax is taken in powers of two
 };
 
+// A long sequence is read in parts of `chunk` tokens by workgroups of their own (at most `parts` of them, the last one takes
+// what is left).  A row that sees one part only is written at once; of the others every part leaves its maximum, sum and
+// output, which sqp_attention_combine joins.  A partial result is D + 4 floats: the output, the maximum, the sum.
+struct SqpParts {
+    int chunk, parts;
+    int pitch;      // partial results per row
+    float *part;
+    __host__ __device__ int of(int sees) const
+    {
+        const int n = sees <= chunk ? 1 : (sees + chunk - 1) / chunk;
+        return n < parts ? n : parts;
+    }
+};
+
+// Sequences whose new tokens make at most this many rows per cached head are for the few-rows kernel (one tile of the
+// 16-column matrix instruction), the others for the tile kernel.  A kernel that is launched alone serves all of them: the few-rows
+// kernel those of up to `most_rows` rows, the tile kernel those of more than `above_rows`.
+constexpr int SQP_FEW_ROWS = 16;
+constexpr int SQP_TILE_ROWS = 128;
+
+void sqp_attention_few(int type, int D, const SqpAttention &a, const SqpParts &p, int most_rows, hipStream_t stream);
+void sqp_attention_tiles(int type, int D, const SqpAttention &a, const SqpParts &p, int above_rows, int max_q, hipStream_t stream);
+
 #ifdef __HIPCC__
 constexpr float SQP_LOWEST = -3e38f;  // the running maximum of a row that has seen nothing: finite, so that differences are
 
 __device__ __forceinline__ float sqp_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <int BYTES> struct SqpWord;
+template <> struct SqpWord<2> { typedef uint16_t t; };
+template <> struct SqpWord<4> { typedef uint32_t t; };
+template <> struct SqpWord<8> { typedef uint2 t; };
+template <> struct SqpWord<16> { typedef uint4 t; };
+
+// Words i of two tokens' values to the pairs (token, next token) of fp16 values: 2 dimensions per word (fp16), 4 (codes).
+template <int TYPE>
+__device__ __forceinline__ void sqp_pair_up(uint32_t a, uint32_t b, uint32_t *pairs)
+{
+    if constexpr (TYPE == SQP_FP16) {
+        pairs[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        pairs[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    } else if constexpr (TYPE == SQP_E4M3) {
+        const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05010400u), hi = __builtin_amdgcn_perm(b, a, 0x07030602u);
+        pairs[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, false));
+        pairs[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, true));
+        pairs[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, false));
+        pairs[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, true));
+    } else {
+        const h16x2 off = {(h16)1152.0f, (h16)1152.0f};
+        const uint32_t sel[4] = {0x0c040c00u, 0x0c050c01u, 0x0c060c02u, 0x0c070c03u};
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            pairs[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, __builtin_amdgcn_perm(b, a, sel[i]) ^ 0x64806480u) - off);
+    }
+}
+
+// Whether a word holds a value that is not finite.
+template <int TYPE>
+__device__ __forceinline__ bool sqp_not_finite(uint32_t w)
+{
+    if constexpr (TYPE == SQP_FP16) return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
+    if constexpr (TYPE == SQP_E4M3)
+        return (w & 0x7fu) == 0x7fu || (w & 0x7f00u) == 0x7f00u || (w & 0x7f0000u) == 0x7f0000u || (w & 0x7f000000u) == 0x7f000000u;
+    return false;
+}
 
 // The new tokens of a sequence, its length in the cache.  What the device arrays say is kept inside the tensors.
 struct SqpSequence {
@@ -65,6 +126,15 @@ __device__ __forceinline__ size_t sqp_cache_row(const SqpAttention &a, const int
 {
     const size_t block = (size_t)sqp_page(a, table_row, token) * a.kv_heads + kv_head;
     return (block << a.page_shift) + (token & ((1 << a.page_shift) - 1));
+}
+
+// Where a row's result of one part goes; false: this part has nothing of the row.
+template <int D>
+__device__ __forceinline__ bool sqp_target(const SqpParts &p, int sees, int part, long row, float *&partial)
+{
+    const int n = p.of(sees);
+    partial = n > 1 ? p.part + ((size_t)row * p.pitch + part) * (D + 4) : nullptr;
+    return part < n;
 }
 
 // One query row over the keys lo .. hi - 1, by one wave: a lane takes every 64th key's score, and D / 64 values of the
@@ -140,6 +210,44 @@ __device__ __forceinline__ void sqp_attend_row(const SqpAttention &a, const h16 
                 if constexpr (PER == 2) o[1] += pj * (float)x.y;
             }
         }
+    }
+}
+
+// The same for a row of a part, result included: the slow way of the kernels below where a value that only some of their rows
+// see is infinite or NaN (zero times it is not zero, so the matrix instructions cannot mask it).
+template <int TYPE, int D>
+__device__ __forceinline__ void sqp_attend_row_of_part(const SqpAttention &a, const SqpParts &parts, int part, int token, int head, int sees, const int *table_row, int lo,
+                                                       int hi)
+{
+    constexpr int PER = D / 64;
+    const long row = (long)token * a.heads + head;
+    float *partial, m, l, o[PER];
+    if (!sqp_target<D>(parts, sees, part, row, partial)) return;
+    sqp_attend_row<TYPE, D>(a, a.q + token * a.q_stride + head * D, table_row, head / a.group, lo, min(hi, sees), m, l, o);
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int e = 0; e < PER; e++) {
+        if (partial) partial[PER * lane + e] = o[e];
+        else a.out[row * D + PER * lane + e] = (h16)(l == 0.f ? 0.f : o[e] / l);
+    }
+    if (partial && lane == 0) {
+        partial[D] = m;
+        partial[D + 1] = l;
+    }
+}
+
+// Rows in front of the first sequence's and behind the last one's: zeros, written by the workgroups of those sequences.
+template <int D>
+__device__ __forceinline__ void sqp_zero_strays(const SqpAttention &a, int b, int kv_head)
+{
+    if (!a.starts) return;
+    const int width8 = a.group * D / 8, pitch8 = a.heads * D / 8;
+    for (int side = 0; side < 2; side++) {
+        const int from = side == 0 ? 0 : max(min(a.starts[a.B], a.T), 0);
+        const int to = side == 0 ? min(max(a.starts[0], 0), a.T) : a.T;
+        if (b != (side == 0 ? 0 : a.B - 1)) continue;
+        for (long i = threadIdx.x; i < (long)max(to - from, 0) * width8; i += blockDim.x)
+            ((uint4 *)a.out)[(from + i / width8) * pitch8 + kv_head * width8 + i % width8] = make_uint4(0, 0, 0, 0);
     }
 }
 #endif

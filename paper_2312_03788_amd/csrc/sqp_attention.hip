@@ -1,41 +1,106 @@
 // Entry point of the attention over the paged cache: argument checks and launches.
+#include <limits.h>
+
+#include <algorithm>
+
 #include "sqp_attention.h"
 
 int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const void *k_cache, const void *v_cache, const float *k_scales, const float *v_scales);
 
 namespace {
 
-// One wave per query row.
-template <int TYPE, int D>
-__global__ void __launch_bounds__(256) attention_rows_kernel(const SqpAttention a)
+// Joins the parts of the rows that have more than one: a wave per row, a lane per part for the weights, then D / 64 values of the
+// output per lane.
+template <int D>
+__global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttention a, const SqpParts few, const SqpParts tiles, int most_rows)
 {
     constexpr int PER = D / 64;
     const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= (long)a.T * a.heads) return;
-    const int token = __builtin_amdgcn_readfirstlane((int)(row / a.heads)), head = __builtin_amdgcn_readfirstlane((int)(row % a.heads));
-    const int b = __builtin_amdgcn_readfirstlane(sqp_sequence_of(a, token));
-    float m, l = 0.f, o[PER] = {};
-    if (b < a.B) {
-        const SqpSequence s = sqp_sequence(a, b);
-        const int sees = min(s.len, s.len - s.n + (token - s.first) + 1);
-        sqp_attend_row<TYPE, D>(a, a.q + token * a.q_stride + head * D, a.table + b * a.table_stride, head / a.group, 0, sees, m, l, o);
-    }
-    h16 *out = a.out + row * D + PER * (threadIdx.x & 63);
+    const int lane = threadIdx.x & 63, token = (int)(row / a.heads);
+    const int b = sqp_sequence_of(a, token);
+    if (b >= a.B) return;
+    const SqpSequence s = sqp_sequence(a, b);
+    const SqpParts &p = s.n * a.group <= most_rows ? few : tiles;
+    const int n = p.of(s.len - s.n + (token - s.first) + 1);
+    if (n == 1) return;
+    const float *part = p.part + (size_t)row * p.pitch * (D + 4);
+    const float m = lane < n ? part[lane * (D + 4) + D] : SQP_LOWEST;
+    float top = m;
 #pragma unroll
-    for (int e = 0; e < PER; e++) out[e] = (h16)(l == 0.f ? 0.f : o[e] / l);
+    for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    const float w = lane < n ? sqp_exp2(m - top) : 0.f;
+    float sum = lane < n ? w * part[lane * (D + 4) + D + 1] : 0.f;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    float o[PER] = {};
+    for (int i = 0; i < n; i += 8) {
+        float x[8][PER];
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+#pragma unroll
+            for (int e = 0; e < PER; e++) x[j][e] = part[min(i + j, n - 1) * (D + 4) + PER * lane + e];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const float wj = __shfl(w, i + j, 64);  // (no weight past the last part)
+#pragma unroll
+            for (int e = 0; e < PER; e++) o[e] += i + j < n ? wj * x[j][e] : 0.f;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < PER; e++) a.out[row * D + PER * lane + e] = (h16)(sum == 0.f ? 0.f : o[e] / sum);
 }
 
-template <int TYPE, int D>
-void rows(const SqpAttention &a, hipStream_t st)
+// What a call launches.
+struct Plan {
+    bool few, tiles;    // which kernels
+    SqpParts f, t;      // their parts (pitch: of both, 1 if nothing is split)
+    int max_q;
+    size_t bytes;       // of partial results
+};
+
+constexpr int MOST_PARTS = 64;  // a lane each when they are joined
+
+SqpParts split(long groups, long wanted, int least, int max_len, int most_parts)
 {
-    attention_rows_kernel<TYPE, D><<<(unsigned)(((long)a.T * a.heads + 3) / 4), 256, 0, st>>>(a);
+    const long parts = std::max(1L, std::min((long)most_parts, wanted / std::max(groups, 1L)));
+    SqpParts p = {};
+    const long chunk = std::max((long)least, (((long)max_len + parts - 1) / parts + 127) / 128 * 128);
+    p.chunk = (int)std::min(chunk, 1L << 30);
+    p.parts = (int)std::max(1L, std::min((long)most_parts, ((long)max_len + chunk - 1) / chunk));
+    return p;
+}
+
+Plan plan(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len, int most_parts)
+{
+    Plan p = {};
+    const int group = heads / kv_heads;
+    p.max_q = std::max(1, std::min(max_q > 0 ? max_q : T, T));
+    max_len = std::max(max_len, 1);
+    const long rows = (long)p.max_q * group;
+    p.few = rows <= SQP_FEW_ROWS || (group <= SQP_FEW_ROWS && (long)B * p.max_q > T);
+    p.tiles = rows > SQP_FEW_ROWS;
+    const long tiles = ((long)T * group + SQP_TILE_ROWS - 1) / SQP_TILE_ROWS;
+    p.f = split((long)B * kv_heads, 1024, 256, max_len, most_parts);
+    p.t = split(tiles * kv_heads, 768, 512, max_len, most_parts);
+    const int pitch = std::max(p.few ? p.f.parts : 1, p.tiles ? p.t.parts : 1);
+    p.f.pitch = p.t.pitch = pitch;
+    p.bytes = pitch > 1 ? (size_t)T * heads * pitch * (D + 4) * sizeof(float) : 0;
+    return p;
+}
+
+template <int D>
+void combine(const SqpAttention &a, const Plan &p, int most_rows, hipStream_t st)
+{
+    attention_combine_kernel<D><<<(unsigned)(((long)a.T * a.heads + 3) / 4), 256, 0, st>>>(a, p.f, p.t, most_rows);
 }
 
 }  // namespace
 
 extern "C" size_t sqp_paged_attention_scratch_bytes(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len)
 {
-    return 0;
+    if (T <= 0 || B <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || max_q < 0 || max_len < 0 || (D != 64 && D != 128)) return 0;
+    return plan(T, B, heads, kv_heads, D, max_q, max_len, MOST_PARTS).bytes;
 }
 
 extern "C" int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D, int type, int page, int pages, int table_width, int max_q, int max_len,
@@ -63,10 +128,15 @@ extern "C" int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D,
     a.table = page_table; a.lens = seq_lens; a.starts = q_starts; a.out = (h16 *)out;
     a.scale2 = scale * 1.44269504088896340736f;
     hipStream_t st = (hipStream_t)stream;
-#define ATTEND(TYPE) (D == 128 ? rows<TYPE, 128>(a, st) : rows<TYPE, 64>(a, st))
-    if (type == SQP_FP16) ATTEND(SQP_FP16);
-    else if (type == SQP_INT8) ATTEND(SQP_INT8);
-    else ATTEND(SQP_E4M3);
-#undef ATTEND
+    const int reach = max_len > 0 ? max_len : table_width * page, most_q = q_starts ? max_q : 1;
+    const size_t row_bytes = (size_t)T * heads * (D + 4) * sizeof(float);
+    Plan p = plan(T, B, heads, kv_heads, D, most_q, reach, MOST_PARTS);
+    if (p.bytes > (scratch ? scratch_bytes : 0))
+        p = plan(T, B, heads, kv_heads, D, most_q, reach, scratch ? (int)std::max((size_t)1, scratch_bytes / row_bytes) : 1);
+    p.f.part = p.t.part = (float *)scratch;
+    const int most_rows = !p.few ? -1 : !p.tiles ? INT_MAX : SQP_FEW_ROWS;  // of the few-rows kernel
+    if (p.few) sqp_attention_few(type, D, a, p.f, most_rows, st);
+    if (p.tiles) sqp_attention_tiles(type, D, a, p.t, std::max(most_rows, 0), p.max_q, st);
+    if (p.f.pitch > 1) D == 128 ? combine<128>(a, p, most_rows, st) : combine<64>(a, p, most_rows, st);
     return sqp_launch_status();
 }

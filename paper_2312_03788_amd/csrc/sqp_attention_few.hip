@@ -1,0 +1,251 @@
+// Attention over the paged cache for few rows per cached head: decode steps, a few tokens at a time.  Bound: the bytes of the
+// cache.
+//
+// Four waves of a workgroup share a (sequence, cached head, part) and take 32 tokens of it in turn; nothing passes between them
+// before the end.  Both products run on 16x16x32 matrix instructions with the up to 16 query rows as columns:
+//   S^T = K Q^T   a lane's A operand is 8 values of one key, as they lie in memory (a lane's 16-byte loads: 16 keys x 64 bytes);
+//                 the values' order within D is free as long as Q has the same.
+//   O^T = V^T P^T the columns of S^T are those of P^T, so p goes from one instruction's result to the other's operand
+//                 without leaving its lane: token 4g + j (j < 4) of either 16 is slot (g, j), g the lane's row of 16.  V^T's operand
+//                 wants 8 tokens' values of one dimension in a lane: a lane loads D / 16 dimensions of its 8 tokens (a load of
+//                 16 lanes is a token's whole row) and pairs tokens up with one byte permutation per word.
+// So nothing goes through shared memory but the four waves' results.
+#include "sqp_attention.h"
+
+namespace {
+
+template <int TYPE, int D>
+__global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttention a, const SqpParts parts, int most_rows)
+{
+    constexpr int BYTES = SqpCode<TYPE>::BYTES;
+    constexpr int KL = D * BYTES / 64;       // 16-byte loads per lane and 16 keys
+    constexpr int VW = D * BYTES / 64;       // words per lane and token of V
+    constexpr int DPL = D / 16;              // dimensions per lane of V
+    typedef typename SqpWord<VW * 4>::t VWord;
+    __shared__ float s_o[4][SQP_FEW_ROWS][D + 4];
+    __shared__ float s_m[4][SQP_FEW_ROWS], s_l[4][SQP_FEW_ROWS];
+    __shared__ int s_bad;
+
+    const int kv_head = blockIdx.x, b = blockIdx.y, part = blockIdx.z;
+    if (part == 0) sqp_zero_strays<D>(a, b, kv_head);
+    const SqpSequence s = sqp_sequence(a, b);
+    const int rows = s.n * a.group;
+    if (rows > most_rows) return;
+    const int *table = a.table + b * a.table_stride;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+    const int before = s.len - s.n;  // token i of the new ones sees before + i + 1
+    const int mask = (1 << a.page_shift) - 1;
+    for (int row0 = 0; row0 < rows; row0 += SQP_FEW_ROWS) {  // (once, unless this kernel serves sequences of more rows)
+        const int count = min(rows - row0, SQP_FEW_ROWS), fewest = before + row0 / a.group + 1, most = before + (row0 + count - 1) / a.group + 1;
+        const int nparts = parts.of(most);
+        if (part >= nparts) continue;
+        const int lo = part * parts.chunk, hi = part == nparts - 1 ? most : lo + parts.chunk;
+        const int row = row0 + min(col, count - 1), token = row / a.group, head = kv_head * a.group + row - token * a.group;
+        const int sees = before + token + 1;
+        if (threadIdx.x == 0) s_bad = 0;
+
+        h16x8 qf[D / 32];
+        {
+            const h16 *q = a.q + (size_t)(s.first + token) * a.q_stride + head * D;
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) qf[i] = *(const h16x8 *)(q + (BYTES == 2 ? 32 * i + 8 * g : 64 * (i >> 1) + 16 * g + 8 * (i & 1)));
+        }
+        // Row in the caches of a 16-token block's first token (pages are whole blocks, so all 16 rows are there; a block that
+        // begins past the end reads the last one's).
+        auto block = [&](int t0) {
+            const int t = min(t0, (hi - 1) & ~15);
+            const size_t page = (size_t)sqp_page(a, table, t) * a.kv_heads + kv_head;
+            return (page << a.page_shift) + (t & mask);
+        };
+        uint4 kw[2][KL];
+        VWord vw[8];
+        f32x4 ks[2], vs[2];
+        auto load_k = [&](int base) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const size_t r = block(base + 16 * i);
+                const uint8_t *p = (const uint8_t *)a.k + r * (D * BYTES) + col * (D * BYTES) + 16 * g;
+#pragma unroll
+                for (int j = 0; j < KL; j++) kw[i][j] = *(const uint4 *)(p + 64 * j);
+                if constexpr (TYPE != SQP_FP16) ks[i] = *(const f32x4 *)(a.k_scales + r + 4 * g);
+            }
+        };
+        auto load_v = [&](int base) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const size_t r = block(base + 16 * i);
+                const uint8_t *p = (const uint8_t *)a.v + r * (D * BYTES) + col * (DPL * BYTES);
+#pragma unroll
+                for (int j = 0; j < 4; j++) vw[4 * i + j] = *(const VWord *)(p + (4 * g + j) * (D * BYTES));
+                if constexpr (TYPE != SQP_FP16) vs[i] = *(const f32x4 *)(a.v_scales + r + 4 * g);
+            }
+        };
+
+        float m = SQP_LOWEST, l = 0.f, lv = TYPE == SQP_FP16 ? 0.f : -60.f;
+        f32x4 o[DPL];
+#pragma unroll
+        for (int t = 0; t < DPL; t++) o[t] = (f32x4)(0.f);
+        bool bad = false;
+        int base = lo + 32 * wave;
+        if (base < hi) {
+            load_k(base);
+            load_v(base);
+        }
+        for (; base < hi; base += 128) {
+            float t[8];
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                f32x4 acc = (f32x4)(0.f);
+#pragma unroll
+                for (int j = 0; j < KL; j++) {
+                    if constexpr (TYPE == SQP_FP16) {
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, kw[i][j]), qf[j], acc, 0, 0, 0);
+                    } else {
+                        const uint32_t w[4] = {kw[i][j].x, kw[i][j].y, kw[i][j].z, kw[i][j].w};
+#pragma unroll
+                        for (int e = 0; e < 2; e++) {
+                            h16x2 p[4];
+                            sqp_halves4<TYPE>(w[2 * e], p[0], p[1]);
+                            sqp_halves4<TYPE>(w[2 * e + 1], p[2], p[3]);
+                            const h16x8 x = {p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
+                            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qf[2 * j + e], acc, 0, 0, 0);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 4; r++) t[4 * i + r] = TYPE == SQP_FP16 ? acc[r] * a.scale2 : acc[r] * (ks[i][r] * a.scale2);
+            }
+            const bool more = base + 128 < hi;
+            if (more) load_k(base + 128);
+            float vmax = 0.f;
+            if (base + 32 > fewest) {  // some row does not see all of these tokens
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int key = base + 16 * (i >> 2) + 4 * g + (i & 3);
+                    if (key >= sees) t[i] = -INFINITY;
+                    if (key >= s.len) {  // memory past the length, whatever it holds
+                        vw[i] = VWord{};
+                        if (TYPE != SQP_FP16) vs[i >> 2][i & 3] = 0.f;
+                    }
+                    if (s.n > 1 && key >= fewest && key < s.len) {
+                        uint32_t w[VW];
+                        __builtin_memcpy(w, &vw[i], sizeof(w));
+#pragma unroll
+                        for (int e = 0; e < VW; e++) bad = bad || sqp_not_finite<TYPE>(w[e]);
+                        if constexpr (TYPE != SQP_FP16) bad = bad || !(__builtin_fabsf(vs[i >> 2][i & 3]) < INFINITY);
+                    }
+                }
+            }
+            float top = t[0];
+#pragma unroll
+            for (int i = 1; i < 8; i++) top = fmaxf(top, t[i]);
+            if constexpr (TYPE != SQP_FP16) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) vmax = fmaxf(vmax, __builtin_fabsf(vs[i >> 2][i & 3]));
+            }
+            // p 2^-lv times a value's scale stays below 2^12 and the largest above 2^-5: inside fp16's range, with the running
+            // maximum (in which lv, the logarithm of the largest scale, is counted) changed only now and then.
+            if (__any(top + lv > m + 12.f || (TYPE != SQP_FP16 && vmax > sqp_exp2(lv)))) {
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                if constexpr (TYPE != SQP_FP16) {
+                    vmax = fmaxf(vmax, __shfl_xor(vmax, 16, 64));
+                    vmax = fmaxf(vmax, __shfl_xor(vmax, 32, 64));
+                    lv = fmaxf(lv, ceilf(__builtin_amdgcn_logf(vmax)));
+                }
+                const float next = top + lv > m + 12.f ? top + lv - 4.f : m, keep = sqp_exp2(m - next);
+                m = next;
+                l *= keep;
+#pragma unroll
+                for (int d = 0; d < DPL; d++) o[d] *= keep;
+            }
+            h16x8 pf;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float p = sqp_exp2(t[i] - m);
+                l += p;
+                pf[i] = (h16)(TYPE == SQP_FP16 ? p : p * vs[i >> 2][i & 3]);
+            }
+            uint32_t pairs[4][DPL];  // [pair of tokens][dimension]
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                uint32_t x[VW], y[VW];
+                __builtin_memcpy(x, &vw[2 * j], sizeof(x));
+                __builtin_memcpy(y, &vw[2 * j + 1], sizeof(y));
+#pragma unroll
+                for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(x[e], y[e], &pairs[j][e * (4 / BYTES)]);
+            }
+            if (more) load_v(base + 128);
+#pragma unroll
+            for (int d = 0; d < DPL; d++) {
+                const u32x4 x = {pairs[0][d], pairs[1][d], pairs[2][d], pairs[3][d]};
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, x), pf, o[d], 0, 0, 0);
+            }
+        }
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (g == 0) {
+            s_m[wave][col] = m;
+            s_l[wave][col] = l;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+#pragma unroll
+            for (int d = 0; d < DPL; d++) s_o[wave][col][DPL * (4 * g + r) + d] = o[d][r];
+        __syncthreads();
+        if (bad) s_bad = 1;
+        __syncthreads();
+        if (s_bad) {
+            for (int r = row0 + wave; r < row0 + count; r += 4) {
+                const int tk = r / a.group;
+                sqp_attend_row_of_part<TYPE, D>(a, parts, part, s.first + tk, kv_head * a.group + r - tk * a.group, before + tk + 1, table, lo, hi);
+            }
+        }
+        for (int i = s_bad ? count * (D / 4) : (int)threadIdx.x; i < count * (D / 4); i += 256) {
+            const int r = i / (D / 4), d = 4 * (i % (D / 4)), tk = (row0 + r) / a.group;
+            const long at = (long)(s.first + tk) * a.heads + kv_head * a.group + row0 + r - tk * a.group;
+            float *partial;
+            if (!sqp_target<D>(parts, before + tk + 1, part, at, partial)) continue;
+            const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+            float sum = 0.f;
+            f32x4 x = (f32x4)(0.f);
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                const float c = sqp_exp2(s_m[w][r] - top);
+                sum += c * s_l[w][r];
+                x += c * *(const f32x4 *)&s_o[w][r][d];
+            }
+            if (partial) {
+                *(f32x4 *)(partial + d) = x;
+                if (d == 0) {
+                    partial[D] = top;
+                    partial[D + 1] = sum;
+                }
+            } else {
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                h16x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] = (h16)(sum == 0.f ? 0.f : x[e] * inv);
+                *(h16x4 *)(a.out + at * D + d) = y;
+            }
+        }
+        __syncthreads();  // (the results and s_bad are written again for the next rows)
+    }
+}
+
+template <int TYPE, int D>
+void launch(const SqpAttention &a, const SqpParts &p, int most_rows, hipStream_t st)
+{
+    attention_few_kernel<TYPE, D><<<dim3((unsigned)a.kv_heads, (unsigned)a.B, (unsigned)p.parts), 256, 0, st>>>(a, p, most_rows);
+}
+
+}  // namespace
+
+void sqp_attention_few(int type, int D, const SqpAttention &a, const SqpParts &p, int most_rows, hipStream_t st)
+{
+#define FEW(TYPE) (D == 128 ? launch<TYPE, 128>(a, p, most_rows, st) : launch<TYPE, 64>(a, p, most_rows, st))
+    if (type == SQP_FP16) FEW(SQP_FP16);
+    else if (type == SQP_INT8) FEW(SQP_INT8);
+    else FEW(SQP_E4M3);
+#undef FEW
+}

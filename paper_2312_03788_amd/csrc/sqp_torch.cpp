@@ -579,7 +579,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     long dev;
     void *stream;
     if (n != 14 || !g_attention || !place(a, n, dev, stream)) Py_RETURN_NONE;
-    const long max_q = a[8] == Py_None ? 0 : PyLong_AsLong(a[8]), max_len = a[9] == Py_None ? 0 : PyLong_AsLong(a[9]);
+    const long max_q = a[5] == Py_None ? 1 : a[8] == Py_None ? 0 : PyLong_AsLong(a[8]), max_len = a[9] == Py_None ? 0 : PyLong_AsLong(a[9]);
     const double given = a[10] == Py_None ? 0.0 : PyFloat_AsDouble(a[10]);
     if (PyErr_Occurred()) {
         PyErr_Clear();
