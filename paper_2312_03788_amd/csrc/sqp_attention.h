@@ -47,11 +47,28 @@ constexpr float SQP_LOWEST = -3e38f;  // the running maximum of a row that has s
 
 __device__ __forceinline__ float sqp_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <int BYTES> struct SqpWord;
-template <> struct SqpWord<2> { typedef uint16_t t; };
-template <> struct SqpWord<4> { typedef uint32_t t; };
-template <> struct SqpWord<8> { typedef uint2 t; };
-template <> struct SqpWord<16> { typedef uint4 t; };
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// BYTES bytes as words.
+template <int BYTES>
+__device__ __forceinline__ void sqp_words(const void *p, uint32_t *w)
+{
+    if constexpr (BYTES == 2) {
+        w[0] = *(const uint16_t *)p;
+    } else if constexpr (BYTES == 4) {
+        w[0] = *(const uint32_t *)p;
+    } else if constexpr (BYTES == 8) {
+        const u32x2 v = *(const u32x2 *)p;
+        w[0] = v.x;
+        w[1] = v.y;
+    } else {
+        const u32x4 v = *(const u32x4 *)p;
+        w[0] = v.x;
+        w[1] = v.y;
+        w[2] = v.z;
+        w[3] = v.w;
+    }
+}
 
 // Words i of two tokens' values to the pairs (token, next token) of fp16 values: 2 dimensions per word (fp16), 4 (codes).
 template <int TYPE>

@@ -21,7 +21,6 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
     constexpr int KL = D * BYTES / 64;       // 16-byte loads per lane and 16 keys
     constexpr int VW = D * BYTES / 64;       // words per lane and token of V
     constexpr int DPL = D / 16;              // dimensions per lane of V
-    typedef typename SqpWord<VW * 4>::t VWord;
     __shared__ float s_o[4][SQP_FEW_ROWS][D + 4];
     __shared__ float s_m[4][SQP_FEW_ROWS], s_l[4][SQP_FEW_ROWS];
     __shared__ int s_bad;
@@ -57,8 +56,8 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             const size_t page = (size_t)sqp_page(a, table, t) * a.kv_heads + kv_head;
             return (page << a.page_shift) + (t & mask);
         };
-        uint4 kw[2][KL];
-        VWord vw[8];
+        u32x4 kw[2][KL];
+        uint32_t vw[8][VW];
         f32x4 ks[2], vs[2];
         auto load_k = [&](int base) {
 #pragma unroll
@@ -66,7 +65,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                 const size_t r = block(base + 16 * i);
                 const uint8_t *p = (const uint8_t *)a.k + r * (D * BYTES) + col * (D * BYTES) + 16 * g;
 #pragma unroll
-                for (int j = 0; j < KL; j++) kw[i][j] = *(const uint4 *)(p + 64 * j);
+                for (int j = 0; j < KL; j++) kw[i][j] = *(const u32x4 *)(p + 64 * j);
                 if constexpr (TYPE != SQP_FP16) ks[i] = *(const f32x4 *)(a.k_scales + r + 4 * g);
             }
         };
@@ -76,7 +75,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                 const size_t r = block(base + 16 * i);
                 const uint8_t *p = (const uint8_t *)a.v + r * (D * BYTES) + col * (DPL * BYTES);
 #pragma unroll
-                for (int j = 0; j < 4; j++) vw[4 * i + j] = *(const VWord *)(p + (4 * g + j) * (D * BYTES));
+                for (int j = 0; j < 4; j++) sqp_words<4 * VW>(p + (4 * g + j) * (D * BYTES), vw[4 * i + j]);
                 if constexpr (TYPE != SQP_FP16) vs[i] = *(const f32x4 *)(a.v_scales + r + 4 * g);
             }
         };
@@ -124,14 +123,13 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                     const int key = base + 16 * (i >> 2) + 4 * g + (i & 3);
                     if (key >= sees) t[i] = -INFINITY;
                     if (key >= s.len) {  // memory past the length, whatever it holds
-                        vw[i] = VWord{};
+#pragma unroll
+                        for (int e = 0; e < VW; e++) vw[i][e] = 0;
                         if (TYPE != SQP_FP16) vs[i >> 2][i & 3] = 0.f;
                     }
                     if (s.n > 1 && key >= fewest && key < s.len) {
-                        uint32_t w[VW];
-                        __builtin_memcpy(w, &vw[i], sizeof(w));
 #pragma unroll
-                        for (int e = 0; e < VW; e++) bad = bad || sqp_not_finite<TYPE>(w[e]);
+                        for (int e = 0; e < VW; e++) bad = bad || sqp_not_finite<TYPE>(vw[i][e]);
                         if constexpr (TYPE != SQP_FP16) bad = bad || !(__builtin_fabsf(vs[i >> 2][i & 3]) < INFINITY);
                     }
                 }
@@ -169,11 +167,8 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             uint32_t pairs[4][DPL];  // [pair of tokens][dimension]
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                uint32_t x[VW], y[VW];
-                __builtin_memcpy(x, &vw[2 * j], sizeof(x));
-                __builtin_memcpy(y, &vw[2 * j + 1], sizeof(y));
 #pragma unroll
-                for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(x[e], y[e], &pairs[j][e * (4 / BYTES)]);
+                for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(vw[2 * j][e], vw[2 * j + 1][e], &pairs[j][e * (4 / BYTES)]);
             }
             if (more) load_v(base + 128);
 #pragma unroll

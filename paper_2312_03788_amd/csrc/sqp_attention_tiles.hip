@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
     constexpr int KP = KU / 4;               // of them per lane (a wave stages 16 tokens)
     constexpr int VD = D / 32;               // dimensions per lane of V
     constexpr int VB = VD * BYTES;           // bytes of them per token
-    typedef typename SqpWord<VB>::t VWord;
+    constexpr int VW = (VB + 3) / 4;         // words of them
     __shared__ __attribute__((aligned(16))) h16 s_k[2][64 * D];
     __shared__ __attribute__((aligned(16))) h16 s_v[2][64 * D];
     __shared__ __attribute__((aligned(16))) float s_ks[2][64], s_vs[2][64];
@@ -57,18 +57,18 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
 #pragma unroll
         for (int c = 0; c < D / 16; c++) qf[c] = *(const h16x8 *)(q + 16 * c);
 
-        uint4 kw[KP];
-        VWord vw[8];
+        u32x4 kw[KP];
+        uint32_t vw[8][VW];
         float kscale = 0.f, vscale = 0.f;
         auto load = [&](int base) {  // a wave: the 16 tokens base + 16 wave ..
             const int t = min(base + 16 * wave, (hi - 1) & ~15);
             const size_t r = (((size_t)sqp_page(a, table, t) * a.kv_heads + kv_head) << a.page_shift) + (t & mask);
             const uint8_t *kp = (const uint8_t *)a.k + r * (D * BYTES) + lane * 16;
 #pragma unroll
-            for (int i = 0; i < KP; i++) kw[i] = *(const uint4 *)(kp + 1024 * i);
+            for (int i = 0; i < KP; i++) kw[i] = *(const u32x4 *)(kp + 1024 * i);
             const uint8_t *vp = (const uint8_t *)a.v + r * (D * BYTES) + 4 * h * (D * BYTES) + col * VB;
 #pragma unroll
-            for (int j = 0; j < 8; j++) vw[j] = *(const VWord *)(vp + (8 * (j >> 2) + (j & 3)) * (D * BYTES));
+            for (int j = 0; j < 8; j++) sqp_words<VB>(vp + (8 * (j >> 2) + (j & 3)) * (D * BYTES), vw[j]);
             if constexpr (TYPE != SQP_FP16) {
                 kscale = a.k_scales[r + (lane & 15)];
                 vscale = a.v_scales[r + (lane & 15)];
@@ -80,13 +80,10 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
 #pragma unroll
                 for (int j = 0; j < 8; j++) {
                     const int key = base + 16 * wave + 8 * (j >> 2) + 4 * h + (j & 3);
-                    if (key >= s.len) {
-                        vw[j] = VWord{};
-                    } else {
-                        uint32_t w[(VB + 3) / 4] = {};
-                        __builtin_memcpy(w, &vw[j], VB);
 #pragma unroll
-                        for (int e = 0; e < (VB + 3) / 4; e++) bad = bad || sqp_not_finite<TYPE>(w[e]);
+                    for (int e = 0; e < VW; e++) {
+                        if (key >= s.len) vw[j][e] = 0;
+                        else bad = bad || sqp_not_finite<TYPE>(vw[j][e]);
                     }
                 }
                 if constexpr (TYPE != SQP_FP16) {
@@ -98,7 +95,7 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
             for (int i = 0; i < KP; i++) {
                 const int unit = lane + 64 * i, key = 16 * wave + unit / KU, piece = unit % KU;
                 if constexpr (TYPE == SQP_FP16) {
-                    *(uint4 *)&s_k[buf][key * D + 8 * (piece ^ (key & (D / 8 - 1)))] = kw[i];
+                    *(u32x4 *)&s_k[buf][key * D + 8 * (piece ^ (key & (D / 8 - 1)))] = kw[i];
                 } else {
                     const uint32_t w[4] = {kw[i].x, kw[i].y, kw[i].z, kw[i].w};
 #pragma unroll
@@ -114,11 +111,8 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
             uint32_t pairs[4][VB < 4 ? 4 : VD];
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                uint32_t x[(VB + 3) / 4] = {}, y[(VB + 3) / 4] = {};
-                __builtin_memcpy(x, &vw[2 * j], VB);
-                __builtin_memcpy(y, &vw[2 * j + 1], VB);
 #pragma unroll
-                for (int e = 0; e < (VB + 3) / 4; e++) sqp_pair_up<TYPE>(x[e], y[e], &pairs[j][e * (4 / BYTES)]);
+                for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(vw[2 * j][e], vw[2 * j + 1][e], &pairs[j][e * (4 / BYTES)]);
             }
 #pragma unroll
             for (int d = 0; d < VD; d++) {
@@ -147,6 +141,9 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
             load(lo);
             store(lo, 0);
         }
+        // Q's loads end here: left to the loop, the wait for them would also be one for the next tile's loads, in every round.
+#pragma unroll
+        for (int c = 0; c < D / 16; c++) asm volatile("" : "+v"(qf[c]));
         int buf = 0;
         for (int base = lo; base < hi; base += 64, buf ^= 1) {
             __syncthreads();
@@ -165,15 +162,17 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
                     }
                 }
                 // result register r of block i: token base + 32 i + 8 (r >> 2) + 4 h + (r & 3)
+                // (fp16: scores are scaled as p is formed)
+                if constexpr (TYPE != SQP_FP16) {
 #pragma unroll
-                for (int i = 0; i < 2; i++)
+                    for (int i = 0; i < 2; i++)
 #pragma unroll
-                    for (int r4 = 0; r4 < 4; r4++) {
-                        f32x4 ks = (f32x4)(a.scale2);
-                        if constexpr (TYPE != SQP_FP16) ks = *(const f32x4 *)&s_ks[buf][32 * i + 8 * r4 + 4 * h];
+                        for (int r4 = 0; r4 < 4; r4++) {
+                            const f32x4 ks = *(const f32x4 *)&s_ks[buf][32 * i + 8 * r4 + 4 * h];
 #pragma unroll
-                        for (int e = 0; e < 4; e++) t[i][4 * r4 + e] *= ks[e];
-                    }
+                            for (int e = 0; e < 4; e++) t[i][4 * r4 + e] *= ks[e];
+                        }
+                }
                 if (base + 64 > wave_least) {
 #pragma unroll
                     for (int i = 0; i < 2; i++)
@@ -184,6 +183,7 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
                 float top = t[0][0];
 #pragma unroll
                 for (int r = 1; r < 32; r++) top = fmaxf(top, t[r >> 4][r & 15]);
+                if constexpr (TYPE == SQP_FP16) top *= a.scale2;
                 float tile_lv = lv;
                 if constexpr (TYPE != SQP_FP16) {
                     const f32x4 x = *(const f32x4 *)s_lv[buf];
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
                         if constexpr (TYPE != SQP_FP16) vs = *(const f32x4 *)&s_vs[buf][32 * i + 8 * r4 + 4 * h];
 #pragma unroll
                         for (int e = 0; e < 4; e++) {
-                            const float p = sqp_exp2(t[i][4 * r4 + e] - m);
+                            const float p = sqp_exp2(TYPE == SQP_FP16 ? __builtin_fmaf(t[i][4 * r4 + e], a.scale2, -m) : t[i][4 * r4 + e] - m);
                             l += p;
                             pf[2 * i + (r4 >> 1)][4 * (r4 & 1) + e] = (h16)(TYPE == SQP_FP16 ? p : p * vs[e]);
                         }
