@@ -20,6 +20,7 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
     constexpr int BYTES = SqpCode<TYPE>::BYTES;
     constexpr int KU = D * BYTES / 16;       // 16-byte pieces per token of K
     constexpr int KP = KU / 4;               // of them per lane (a wave stages 16 tokens)
+    constexpr int AHEAD = 4;                 // operands fetched ahead of the matrix instructions
     constexpr int VD = D / 32;               // dimensions per lane of V
     constexpr int VB = VD * BYTES;           // bytes of them per token
     constexpr int VW = (VB + 3) / 4;         // words of them
@@ -60,9 +61,13 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
         u32x4 kw[KP];
         uint32_t vw[8][VW];
         float kscale = 0.f, vscale = 0.f;
-        auto load = [&](int base) {  // a wave: the 16 tokens base + 16 wave ..
-            const int t = min(base + 16 * wave, (hi - 1) & ~15);
-            const size_t r = (((size_t)sqp_page(a, table, t) * a.kv_heads + kv_head) << a.page_shift) + (t & mask);
+        // A wave stages the 16 tokens base + 16 wave ..; their page is looked up a tile ahead.
+        auto place = [&](int base) { return min(base + 16 * wave, (hi - 1) & ~15); };
+        int page = lo < hi ? sqp_page(a, table, place(lo)) : 0;
+        auto load = [&](int base) {
+            const int t = place(base);
+            const size_t r = (((size_t)__builtin_amdgcn_readfirstlane(page) * a.kv_heads + kv_head) << a.page_shift) + (t & mask);
+            page = sqp_page(a, table, place(base + 64));
             const uint8_t *kp = (const uint8_t *)a.k + r * (D * BYTES) + lane * 16;
 #pragma unroll
             for (int i = 0; i < KP; i++) kw[i] = *(const u32x4 *)(kp + 1024 * i);
@@ -150,28 +155,46 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
             const bool more = base + 64 < hi;
             if (more) load(base + 64);
             if (base < wave_most) {
+                // The order of instructions is fixed: the compiler's own waits for every operand as soon as it is asked for.
+                // Operands are fetched four matrix instructions ahead, and what has to be done to the first 32 tokens' scores is
+                // done beside the next 32's products.
                 f32x16 t[2];
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    t[i] = (f32x16)(0.f);
-                    const int key = 32 * i + col;
-#pragma unroll
-                    for (int c = 0; c < D / 16; c++) {
-                        const h16x8 k = *(const h16x8 *)&s_k[buf][key * D + 8 * ((2 * c + h) ^ (key & (D / 8 - 1)))];
-                        t[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[c], t[i], 0, 0, 0);
-                    }
-                }
+                t[0] = t[1] = (f32x16)(0.f);
+                h16x8 kf[AHEAD];
+                f32x4 ks[4];
+                auto fetch_k = [&](int n) {
+                    const int key = 32 * (n / (D / 16)) + col, c = n % (D / 16);
+                    kf[n % AHEAD] = *(const h16x8 *)&s_k[buf][key * D + 8 * ((2 * c + h) ^ (key & (D / 8 - 1)))];
+                };
                 // result register r of block i: token base + 32 i + 8 (r >> 2) + 4 h + (r & 3)
-                // (fp16: scores are scaled as p is formed)
+                auto fetch_ks = [&](int i, int r4) { ks[r4] = *(const f32x4 *)&s_ks[buf][32 * i + 8 * r4 + 4 * h]; };
+                auto scale = [&](int i, int r4) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) t[i][4 * r4 + e] *= ks[r4][e];
+                };
+#pragma unroll
+                for (int n = 0; n < AHEAD; n++) fetch_k(n);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int n = 0; n < D / 8; n++) {
+                    t[n / (D / 16)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[n % AHEAD], qf[n % (D / 16)], t[n / (D / 16)], 0, 0, 0);
+                    if (n + AHEAD < D / 8) fetch_k(n + AHEAD);
+                    if constexpr (TYPE != SQP_FP16) {  // (fp16: scores are scaled as p is formed)
+                        const int j = n - D / 16;
+                        if (j >= 0 && j < 4) fetch_ks(0, j);
+                        if (j == D / 16 - 1) {
+#pragma unroll
+                            for (int r4 = 0; r4 < 4; r4++) {
+                                scale(0, r4);
+                                fetch_ks(1, r4);
+                            }
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
                 if constexpr (TYPE != SQP_FP16) {
 #pragma unroll
-                    for (int i = 0; i < 2; i++)
-#pragma unroll
-                        for (int r4 = 0; r4 < 4; r4++) {
-                            const f32x4 ks = *(const f32x4 *)&s_ks[buf][32 * i + 8 * r4 + 4 * h];
-#pragma unroll
-                            for (int e = 0; e < 4; e++) t[i][4 * r4 + e] *= ks[e];
-                        }
+                    for (int r4 = 0; r4 < 4; r4++) scale(1, r4);
                 }
                 if (base + 64 > wave_least) {
 #pragma unroll
@@ -199,28 +222,45 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
                     for (int d = 0; d < D / 32; d++) o[d] *= keep;
                 }
                 lv = tile_lv;
-                h16x8 pf[4];
-#pragma unroll
-                for (int i = 0; i < 2; i++)
-#pragma unroll
-                    for (int r4 = 0; r4 < 4; r4++) {
-                        f32x4 vs = (f32x4)(1.f);
-                        if constexpr (TYPE != SQP_FP16) vs = *(const f32x4 *)&s_vs[buf][32 * i + 8 * r4 + 4 * h];
-#pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const float p = sqp_exp2(TYPE == SQP_FP16 ? __builtin_fmaf(t[i][4 * r4 + e], a.scale2, -m) : t[i][4 * r4 + e] - m);
-                            l += p;
-                            pf[2 * i + (r4 >> 1)][4 * (r4 & 1) + e] = (h16)(TYPE == SQP_FP16 ? p : p * vs[e]);
-                        }
+                // p of step c + 1 is formed beside the matrix instructions of step c
+                h16x8 pf[2], vf[AHEAD];
+                f32x4 vs[2];
+                auto fetch_v = [&](int n) {
+                    const int c = n / (D / 32), dim = 32 * (n % (D / 32)) + col;
+                    vf[n % AHEAD] = *(const h16x8 *)&s_v[buf][dim * 64 + 8 * ((2 * c + h) ^ ((dim ^ (dim >> 2)) & 7))];
+                };
+                auto fetch_vs = [&](int c) {
+                    if constexpr (TYPE != SQP_FP16) {
+                        vs[0] = *(const f32x4 *)&s_vs[buf][16 * c + 4 * h];
+                        vs[1] = *(const f32x4 *)&s_vs[buf][16 * c + 8 + 4 * h];
                     }
+                };
+                auto form = [&](int c, int from, int to) {
 #pragma unroll
-                for (int c = 0; c < 4; c++)
-#pragma unroll
-                    for (int d = 0; d < D / 32; d++) {
-                        const int dim = 32 * d + col;
-                        const h16x8 v = *(const h16x8 *)&s_v[buf][dim * 64 + 8 * ((2 * c + h) ^ ((dim ^ (dim >> 2)) & 7))];
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[c], o[d], 0, 0, 0);
+                    for (int j = from; j < to; j++) {
+                        const float x = t[c >> 1][8 * (c & 1) + j];
+                        const float p = sqp_exp2(TYPE == SQP_FP16 ? __builtin_fmaf(x, a.scale2, -m) : x - m);
+                        l += p;
+                        pf[c & 1][j] = (h16)(TYPE == SQP_FP16 ? p : p * vs[j >> 2][j & 3]);
                     }
+                };
+                fetch_vs(0);
+#pragma unroll
+                for (int n = 0; n < AHEAD; n++) fetch_v(n);
+                __builtin_amdgcn_sched_barrier(0);
+                form(0, 0, 8);
+                fetch_vs(1);
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int ND = D / 32, SHARE = 8 / ND;
+#pragma unroll
+                for (int n = 0; n < 4 * ND; n++) {
+                    const int c = n / ND, d = n % ND;
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n % AHEAD], pf[c & 1], o[d], 0, 0, 0);
+                    if (n + AHEAD < 4 * ND) fetch_v(n + AHEAD);
+                    if (c < 3) form(c + 1, SHARE * d, SHARE * (d + 1));
+                    if (c < 2 && d == ND - 1) fetch_vs(c + 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             if (more) store(base + 64, buf ^ 1);
         }
