@@ -37,10 +37,9 @@ struct SqpParts {
 // 16-column matrix instruction), the others for the tile kernel.  A kernel that is launched alone serves all of them: the few-rows
 // kernel those of up to `most_rows` rows, the tile kernel those of more than `above_rows`.
 constexpr int SQP_FEW_ROWS = 16;
-constexpr int SQP_TILE_ROWS = 128;
 
 void sqp_attention_few(int type, int D, const SqpAttention &a, const SqpParts &p, int most_rows, hipStream_t stream);
-void sqp_attention_tiles(int type, int D, const SqpAttention &a, const SqpParts &p, int above_rows, int max_q, hipStream_t stream);
+void sqp_attention_tiles(int type, int D, const SqpAttention &a, const SqpParts &p, int tile_rows, int above_rows, int fold, hipStream_t stream);
 
 #ifdef __HIPCC__
 constexpr float SQP_LOWEST = -3e38f;  // the running maximum of a row that has seen nothing: finite, so that differences are
@@ -53,7 +52,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 template <int BYTES>
 __device__ __forceinline__ void sqp_words(const void *p, uint32_t *w)
 {
-    if constexpr (BYTES == 2) {
+    if constexpr (BYTES == 1) {
+        w[0] = *(const uint8_t *)p;
+    } else if constexpr (BYTES == 2) {
         w[0] = *(const uint16_t *)p;
     } else if constexpr (BYTES == 4) {
         w[0] = *(const uint32_t *)p;
@@ -89,6 +90,22 @@ __device__ __forceinline__ void sqp_pair_up(uint32_t a, uint32_t b, uint32_t *pa
 #pragma unroll
         for (int i = 0; i < 4; i++)
             pairs[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, __builtin_amdgcn_perm(b, a, sel[i]) ^ 0x64806480u) - off);
+    }
+}
+
+// One of those pairs: dimension d of the tokens' words a, b.
+template <int TYPE>
+__device__ __forceinline__ uint32_t sqp_pair(const uint32_t *a, const uint32_t *b, int d)
+{
+    if constexpr (TYPE == SQP_FP16) {
+        return __builtin_amdgcn_perm(b[d / 2], a[d / 2], d & 1 ? 0x07060302u : 0x05040100u);
+    } else if constexpr (TYPE == SQP_E4M3) {
+        const uint32_t both = __builtin_amdgcn_perm(b[d / 4], a[d / 4], 0x0c0c0400u + 0x0101u * (uint32_t)(d % 4));
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)both, 1.0f, false));
+    } else {
+        const h16x2 off = {(h16)1152.0f, (h16)1152.0f};
+        const uint32_t both = __builtin_amdgcn_perm(b[d / 4], a[d / 4], 0x0c040c00u + 0x00010001u * (uint32_t)(d % 4));
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, both ^ 0x64806480u) - off);
     }
 }
 
@@ -253,18 +270,80 @@ __device__ __forceinline__ void sqp_attend_row_of_part(const SqpAttention &a, co
     }
 }
 
-// Rows in front of the first sequence's and behind the last one's: zeros, written by the workgroups of those sequences.
+// Rows in front of the first sequence's and behind the last one's: zeros.
 template <int D>
-__device__ __forceinline__ void sqp_zero_strays(const SqpAttention &a, int b, int kv_head)
+__device__ __forceinline__ void sqp_zero_strays(const SqpAttention &a, int kv_head)
 {
     if (!a.starts) return;
     const int width8 = a.group * D / 8, pitch8 = a.heads * D / 8;
+    const int front = min(max(a.starts[0], 0), a.T), back = max(min(a.starts[a.B], a.T), 0);
     for (int side = 0; side < 2; side++) {
-        const int from = side == 0 ? 0 : max(min(a.starts[a.B], a.T), 0);
-        const int to = side == 0 ? min(max(a.starts[0], 0), a.T) : a.T;
-        if (b != (side == 0 ? 0 : a.B - 1)) continue;
+        const int from = side == 0 ? 0 : back, to = side == 0 ? front : a.T;
         for (long i = threadIdx.x; i < (long)max(to - from, 0) * width8; i += blockDim.x)
             ((uint4 *)a.out)[(from + i / width8) * pitch8 + kv_head * width8 + i % width8] = make_uint4(0, 0, 0, 0);
     }
+}
+
+// Sum over a wave's lanes (row by row, then across the rows), the same in all of them.
+__device__ __forceinline__ int sqp_wave_sum(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    return __builtin_amdgcn_readlane(x, 15) + __builtin_amdgcn_readlane(x, 31) + __builtin_amdgcn_readlane(x, 47) + __builtin_amdgcn_readlane(x, 63);
+}
+
+// The tile (of `height` rows) that is rank-th in the order of work, over all sequences of more than above_rows rows: those first
+// that see most, so that the long ones do not begin last.  From `fold` on the order is turned round: with as many
+// workgroups as fit the chip at once, the shortest share their compute units with the longest.  b < 0: no such tile.
+struct SqpTile {
+    int b, tile;
+};
+__device__ __forceinline__ SqpTile sqp_pick_tile(const SqpAttention &a, int above_rows, int height, int rank, int fold)
+{
+    const int lane = threadIdx.x & 63;
+    auto tiles_of = [&](int b) {
+        const SqpSequence s = sqp_sequence(a, b);
+        const int rows = s.n * a.group;
+        return rows > above_rows ? (rows + height - 1) / height : 0;
+    };
+    if (a.B > 64) {  // in the sequences' order
+        int first = 0;
+        for (int i = 0; i < a.B; i += 64) {
+            const int n = i + lane < a.B ? tiles_of(i + lane) : 0, all = sqp_wave_sum(n);
+            if (rank < first + all) {
+                for (int j = 0; j < 64; j++) {
+                    const int nj = __builtin_amdgcn_readlane(n, j);
+                    if (rank < first + nj) return {i + j, nj - 1 - (rank - first)};
+                    first += nj;
+                }
+            }
+            first += all;
+        }
+        return {-1, 0};
+    }
+    const int n = lane < a.B ? tiles_of(lane) : 0, all = a.B == 1 ? __builtin_amdgcn_readlane(n, 0) : sqp_wave_sum(n);
+    if (rank >= all) return {-1, 0};
+    if (fold > 0 && rank >= fold) rank = all - 1 - (rank - fold);
+    if (a.B == 1) return {0, all - 1 - rank};
+    // A tile's key: its sequence's length, less a power of two near the tokens per tile for every tile behind it.
+    int shift = 0;
+    while ((a.group << (shift + 1)) <= height) shift++;
+    const int len = lane < a.B ? sqp_sequence(a, lane).len : 0;
+    auto above = [&](int x) {  // tiles of this lane's sequence with a key greater than x
+        return len <= x ? 0 : min(n, ((len - x - 1) >> shift) + 1);
+    };
+    int lo = -(int)((unsigned)a.T << 1) - 1, hi = a.table_width << a.page_shift;  // no key beyond hi, all above lo
+    while (lo < hi) {
+        const int mid = lo + ((hi - lo) >> 1);
+        if (sqp_wave_sum(above(mid)) <= rank) hi = mid;
+        else lo = mid + 1;
+    }
+    const int here = above(lo - 1) - above(lo);  // 1: this lane's sequence has a tile with the key lo
+    unsigned long long who = __ballot(here > 0);
+    for (int skip = rank - sqp_wave_sum(above(lo)); skip > 0; skip--) who &= who - 1;
+    const int b = __ffsll((long long)who) - 1;
+    return {b, __builtin_amdgcn_readlane(n, b) - 1 - __builtin_amdgcn_readlane(above(lo), b)};
 }
 #endif

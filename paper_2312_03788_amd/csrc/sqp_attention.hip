@@ -9,16 +9,16 @@ int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const vo
 
 namespace {
 
-// Joins the parts of the rows that have more than one: a wave per row, a lane per part for the weights, then D / 64 values of the
-// output per lane.
+// Joins the parts of the rows that have more than one: a wave per row, a lane per part for the weights; then D / 4 lanes have four
+// values of a part each, so that two (D = 128) or four parts are read at once.
 template <int D>
 __global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttention a, const SqpParts few, const SqpParts tiles, int most_rows)
 {
-    constexpr int PER = D / 64;
-    const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (long)a.T * a.heads) return;
-    const int lane = threadIdx.x & 63, token = (int)(row / a.heads);
-    const int b = sqp_sequence_of(a, token);
+    constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6);  // (T heads D < 2^31)
+    if (row >= a.T * a.heads) return;
+    const int lane = threadIdx.x & 63, token = __builtin_amdgcn_readfirstlane(row / a.heads);
+    const int b = __builtin_amdgcn_readfirstlane(sqp_sequence_of(a, token));
     if (b >= a.B) return;
     const SqpSequence s = sqp_sequence(a, b);
     const SqpParts &p = s.n * a.group <= most_rows ? few : tiles;
@@ -29,33 +29,41 @@ __global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttenti
     float top = m;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    const float w = lane < n ? sqp_exp2(m - top) : 0.f;
+    const float w = lane < n ? sqp_exp2(m - top) : 0.f;  // (no weight past the last part)
     float sum = lane < n ? w * part[lane * (D + 4) + D + 1] : 0.f;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    float o[PER] = {};
-    for (int i = 0; i < n; i += 8) {
-        float x[8][PER];
+    const int d = 4 * (lane % LANES), which = lane / LANES;
+    f32x4 o = (f32x4)(0.f);
+    for (int i = 0; i < n; i += 4 * AT_ONCE) {
+        f32x4 x[4];
 #pragma unroll
-        for (int j = 0; j < 8; j++)
+        for (int j = 0; j < 4; j++) x[j] = *(const f32x4 *)&part[min(i + j * AT_ONCE + which, n - 1) * (D + 4) + d];
 #pragma unroll
-            for (int e = 0; e < PER; e++) x[j][e] = part[min(i + j, n - 1) * (D + 4) + PER * lane + e];
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const float wj = __shfl(w, i + j, 64);  // (no weight past the last part)
-#pragma unroll
-            for (int e = 0; e < PER; e++) o[e] += i + j < n ? wj * x[j][e] : 0.f;
+        for (int j = 0; j < 4; j++) {
+            const int at = i + j * AT_ONCE + which;
+            const float wj = __shfl(w, at & 63, 64);
+            if (at < n) o += wj * x[j];
         }
     }
 #pragma unroll
-    for (int e = 0; e < PER; e++) a.out[row * D + PER * lane + e] = (h16)(sum == 0.f ? 0.f : o[e] / sum);
+    for (int off = 32; off >= LANES; off >>= 1)
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] += __shfl_xor(o[e], off, 64);
+    if (which == 0) {
+        h16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; e++) y[e] = (h16)(sum == 0.f ? 0.f : o[e] / sum);
+        *(h16x4 *)(a.out + (size_t)row * D + d) = y;
+    }
 }
 
 // What a call launches.
 struct Plan {
     bool few, tiles;    // which kernels
+    int tile_rows;      // 128 or 256
     SqpParts f, t;      // their parts (pitch: of both, 1 if nothing is split)
-    int max_q;
+    int fold;           // tiles on the first half of the places, the shortest then share theirs (0: none)
     size_t bytes;       // of partial results
 };
 
@@ -75,14 +83,22 @@ Plan plan(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len, 
 {
     Plan p = {};
     const int group = heads / kv_heads;
-    p.max_q = std::max(1, std::min(max_q > 0 ? max_q : T, T));
+    max_q = std::max(1, std::min(max_q > 0 ? max_q : T, T));
     max_len = std::max(max_len, 1);
-    const long rows = (long)p.max_q * group;
-    p.few = rows <= SQP_FEW_ROWS || (group <= SQP_FEW_ROWS && (long)B * p.max_q > T);
+    const long rows = (long)max_q * group;
+    // Single tokens beside prompts: the few-rows kernel reads their cache faster, but its launch waits for the other one's end. Up to
+    // 8 sequences the tile kernel takes them along.
+    p.few = rows <= SQP_FEW_ROWS || (group <= SQP_FEW_ROWS && (long)B * max_q > T && B > 8);
     p.tiles = rows > SQP_FEW_ROWS;
-    const long tiles = ((long)T * group + SQP_TILE_ROWS - 1) / SQP_TILE_ROWS;
-    p.f = split((long)B * kv_heads, 1024, 256, max_len, most_parts);
-    p.t = split(tiles * kv_heads, 768, 512, max_len, most_parts);
+    // Tiles of 256 rows are the quicker ones where they fill the chip (a workgroup per compute unit) several times over; tiles
+    // of 128 rows (two per compute unit) spread better.
+    auto count = [&](int height) { return (B == 1 ? ((long)T * group + height - 1) / height : (long)T * group / height + B) * kv_heads; };
+    p.tile_rows = count(256) >= 2 * 256 ? 256 : 128;
+    const long blocks = count(p.tile_rows);
+    p.f = split((long)B * kv_heads, 512, 256, max_len, most_parts);
+    p.t = split(blocks, 512, 512, max_len, most_parts);
+    const int at_once = p.tile_rows == 128 ? 512 : 256;
+    p.fold = blocks * p.t.parts <= at_once && p.tile_rows == 128 ? 256 / (kv_heads * p.t.parts) : 0;
     const int pitch = std::max(p.few ? p.f.parts : 1, p.tiles ? p.t.parts : 1);
     p.f.pitch = p.t.pitch = pitch;
     p.bytes = pitch > 1 ? (size_t)T * heads * pitch * (D + 4) * sizeof(float) : 0;
@@ -92,7 +108,7 @@ Plan plan(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len, 
 template <int D>
 void combine(const SqpAttention &a, const Plan &p, int most_rows, hipStream_t st)
 {
-    attention_combine_kernel<D><<<(unsigned)(((long)a.T * a.heads + 3) / 4), 256, 0, st>>>(a, p.f, p.t, most_rows);
+    attention_combine_kernel<D><<<(unsigned)((a.T * a.heads + 3) / 4), 256, 0, st>>>(a, p.f, p.t, most_rows);
 }
 
 }  // namespace
@@ -136,7 +152,7 @@ extern "C" int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D,
     p.f.part = p.t.part = (float *)scratch;
     const int most_rows = !p.few ? -1 : !p.tiles ? INT_MAX : SQP_FEW_ROWS;  // of the few-rows kernel
     if (p.few) sqp_attention_few(type, D, a, p.f, most_rows, st);
-    if (p.tiles) sqp_attention_tiles(type, D, a, p.t, std::max(most_rows, 0), p.max_q, st);
+    if (p.tiles) sqp_attention_tiles(type, D, a, p.t, p.tile_rows, std::max(most_rows, 0), p.fold, st);
     if (p.f.pitch > 1) D == 128 ? combine<128>(a, p, most_rows, st) : combine<64>(a, p, most_rows, st);
     return sqp_launch_status();
 }

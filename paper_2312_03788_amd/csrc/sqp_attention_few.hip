@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
     __shared__ int s_bad;
 
     const int kv_head = blockIdx.x, b = blockIdx.y, part = blockIdx.z;
-    if (part == 0) sqp_zero_strays<D>(a, b, kv_head);
+    if (part == 0 && b == 0) sqp_zero_strays<D>(a, kv_head);
     const SqpSequence s = sqp_sequence(a, b);
     const int rows = s.n * a.group;
     if (rows > most_rows) return;
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             }
             // p 2^-lv times a value's scale stays below 2^12 and the largest above 2^-5: inside fp16's range, with the running
             // maximum (in which lv, the logarithm of the largest scale, is counted) changed only now and then.
-            if (__any(top + lv > m + 12.f || (TYPE != SQP_FP16 && vmax > sqp_exp2(lv)))) {
+            if (__any(top + lv > m + 15.f || (TYPE != SQP_FP16 && vmax > sqp_exp2(lv)))) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
                 if constexpr (TYPE != SQP_FP16) {
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                     vmax = fmaxf(vmax, __shfl_xor(vmax, 32, 64));
                     lv = fmaxf(lv, ceilf(__builtin_amdgcn_logf(vmax)));
                 }
-                const float next = top + lv > m + 12.f ? top + lv - 4.f : m, keep = sqp_exp2(m - next);
+                const float next = top + lv > m + 15.f ? top + lv : m, keep = sqp_exp2(m - next);
                 m = next;
                 l *= keep;
 #pragma unroll

@@ -1,48 +1,67 @@
 // Attention over the paged cache for many rows per cached head: prompts and chunks of them.  Bound: the matrix cores, and beside
 // them the softmax's vector work.
 //
-// A workgroup takes 128 rows (new token, query head) of one (sequence, cached head, part), a wave 32 of them, and goes through
-// the tokens 64 at a time.  S^T = K Q^T and O^T = V^T P^T on 32x32x16 matrix instructions: a lane has one query row's scores (half
-// of them, the other half in lane ^ 32), so the softmax's row reductions stay in the lane and its p are the second product's operand
-// as they stand: tokens 16c + 8 (j >> 2) + 4h + (j & 3), j = 0..7, are slot (h, j) of its step c, h the lane's half.
-// K and V^T lie in shared memory in fp16 (codes are exact there; their scales are applied to scores and p in fp32), twice, so
-// that the next tile is fetched, converted and transposed while this one is used: one barrier per tile.  V is transposed on the
-// way: a thread holds the 8 tokens of a slot group and pairs them up with byte permutations.
+// A workgroup of W = 4 or 8 waves takes 32 W rows (new token, query head) of one (sequence, cached head, part), a wave 32 of them,
+// and goes through the tokens 64 at a time.  S^T = K Q^T and O^T = V^T P^T on 32x32x16 matrix instructions: a lane has one query
+// row's scores (half of them, the other half in lane ^ 32), so the softmax's row reductions stay in the lane and its p are the
+// second product's operand as they stand: tokens 16c + 8 (j >> 2) + 4h + (j & 3), j = 0..7, are slot (h, j) of its step c, h the
+// lane's half.
+//
+// Work goes in steps of 32 tokens whose order of instructions is fixed (left alone, the compiler waits for every operand as soon
+// as it has asked for it): the next step's scores and this step's output are computed by the matrix cores beside this
+// step's softmax, an exponential or two behind each matrix instruction, operands fetched some instructions ahead.
+//
+// K and V^T lie in shared memory in fp16 (codes are exact there).  The scale of a token's key multiplies its scores in fp32;
+// the scale of its value is part of the exponent, p' = 2^(s + lv - m) with lv its logarithm, and leaves the sum again by its
+// inverse, so that what is rounded to fp16 is the weight of the value's codes and stays inside fp16's range whatever the
+// scales.  V is transposed on the way into shared memory: a thread holds the 8 tokens of a slot and pairs them up with
+// byte permutations.  What is stored between two barriers is read after the second, and values come from memory a whole
+// tile ahead of their storing; with three tiles of V (8 waves) that is one barrier per 64 tokens, with two (4 waves, two
+// workgroups per compute unit) it is two.
 #include <algorithm>
 
 #include "sqp_attention.h"
 
 namespace {
 
-template <int TYPE, int D>
-__global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttention a, const SqpParts parts, int above_rows, int tiles)
+template <int TYPE, int D, int W>
+__global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAttention a, const SqpParts parts, int above_rows, int fold)
 {
-    constexpr int BYTES = SqpCode<TYPE>::BYTES;
-    constexpr int KU = D * BYTES / 16;       // 16-byte pieces per token of K
-    constexpr int KP = KU / 4;               // of them per lane (a wave stages 16 tokens)
-    constexpr int AHEAD = 4;                 // operands fetched ahead of the matrix instructions
-    constexpr int VD = D / 32;               // dimensions per lane of V
-    constexpr int VB = VD * BYTES;           // bytes of them per token
-    constexpr int VW = (VB + 3) / 4;         // words of them
-    __shared__ __attribute__((aligned(16))) h16 s_k[2][64 * D];
-    __shared__ __attribute__((aligned(16))) h16 s_v[2][64 * D];
-    __shared__ __attribute__((aligned(16))) float s_ks[2][64], s_vs[2][64];
-    __shared__ __attribute__((aligned(16))) float s_lv[2][4];
+    constexpr bool CODES = TYPE != SQP_FP16;
+    constexpr int ROWS = 32 * W, BYTES = SqpCode<TYPE>::BYTES;
+    constexpr int TOKENS = 64 / W;                  // that a wave stages
+    constexpr int KU = D * BYTES / 16;              // 16-byte pieces per token of K
+    constexpr int KL = (TOKENS * KU + 63) / 64;     // of them per lane
+    constexpr int KPIECES = KL * (CODES ? 2 : 1);   // its stores
+    constexpr int VD = W == 4 ? D / 32 : D / 64;    // dimensions per lane of V (4 waves: half a wave holds a token, 8 waves: a wave)
+    constexpr int VSUB = D / 32 / VD;               // blocks of 32 rows of V^T per dimension of a lane
+    constexpr int VB = VD * BYTES, VW = (VB + 3) / 4;
+    constexpr int NK = D / 16, NV = D / 32;         // operands per step: of K, of V per 16 tokens
+    constexpr int AHEAD = CODES && W == 4 ? 3 : 4;  // operands fetched ahead (as many as the registers hold)
+    constexpr int KROW = D + 8, VROW = 64 + 8;      // 16 bytes between rows: eight lanes' operands lie in eight different sets of banks
+    constexpr int VBUFS = W == 8 ? 3 : 2;
+    __shared__ __attribute__((aligned(16))) h16 s_k[2][64 * KROW];
+    __shared__ __attribute__((aligned(16))) h16 s_v[VBUFS][D * VROW];
+    __shared__ __attribute__((aligned(16))) float s_ks[2][64], s_lv[2][64], s_rv[VBUFS][64];
     __shared__ int s_bad;
 
-    const int kv_head = blockIdx.x, b = blockIdx.z, part = blockIdx.y % parts.parts;
-    if (blockIdx.y == 0) sqp_zero_strays<D>(a, b, kv_head);
-    const SqpSequence s = sqp_sequence(a, b);
-    const int rows = s.n * a.group;
-    if (rows <= above_rows) return;
-    const int *table = a.table + b * a.table_stride;
+    const int kv_head = blockIdx.x, part = blockIdx.y % parts.parts, ranks = gridDim.y / parts.parts;
+    if (blockIdx.y == 0) sqp_zero_strays<D>(a, kv_head);
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
-    const int before = s.len - s.n;  // token i of the new ones sees before + i + 1
     const int mask = (1 << a.page_shift) - 1;
+    // what this thread stages of a tile: K's tokens first_token .., V's slots (v_half, j) of 16 tokens, dimensions VD v_lane ..
+    const int block16 = TOKENS * wave / 16, first_token = TOKENS * wave % 16;
+    const int v_half = W == 4 ? h : wave & 1, v_lane = W == 4 ? col : lane;
 
-    // the last tiles, which see most, first
-    for (int tile = tiles - 1 - (int)blockIdx.y / parts.parts; tile * SQP_TILE_ROWS < rows; tile += tiles) {
-        const int row0 = tile * SQP_TILE_ROWS, row_last = min(row0 + SQP_TILE_ROWS, rows) - 1;
+    for (int rank = blockIdx.y / parts.parts;; rank += ranks) {  // (once, as long as the starts are in order)
+        const SqpTile at_tile = sqp_pick_tile(a, above_rows, ROWS, rank, fold);
+        const int b = __builtin_amdgcn_readfirstlane(at_tile.b), tile = __builtin_amdgcn_readfirstlane(at_tile.tile);
+        if (b < 0) break;
+        const SqpSequence s = sqp_sequence(a, b);
+        const int rows = s.n * a.group;
+        const int *table = a.table + b * a.table_stride;
+        const int before = s.len - s.n;  // token i of the new ones sees before + i + 1
+        const int row0 = tile * ROWS, row_last = min(row0 + ROWS, rows) - 1;
         const int most = before + row_last / a.group + 1, least = before + row0 / a.group + 1;
         const int nparts = parts.of(most);
         if (part >= nparts) continue;
@@ -53,222 +72,304 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
         const int wave_row = row0 + 32 * wave, wave_least = before + min(wave_row, rows - 1) / a.group + 1;
         const int wave_most = wave_row >= rows ? 0 : before + min(wave_row + 31, rows - 1) / a.group + 1;
 
-        h16x8 qf[D / 16];
-        const h16 *q = a.q + (size_t)(s.first + token) * a.q_stride + head * D + 8 * h;
+        h16x8 qf[NK];
+        auto load_q = [&] {
+            const h16 *q = a.q + (size_t)(s.first + token) * a.q_stride + head * D + 8 * h;
 #pragma unroll
-        for (int c = 0; c < D / 16; c++) qf[c] = *(const h16x8 *)(q + 16 * c);
-
-        u32x4 kw[KP];
-        uint32_t vw[8][VW];
-        float kscale = 0.f, vscale = 0.f;
-        // A wave stages the 16 tokens base + 16 wave ..; their page is looked up a tile ahead.
-        auto place = [&](int base) { return min(base + 16 * wave, (hi - 1) & ~15); };
-        int page = lo < hi ? sqp_page(a, table, place(lo)) : 0;
-        auto load = [&](int base) {
-            const int t = place(base);
-            const size_t r = (((size_t)__builtin_amdgcn_readfirstlane(page) * a.kv_heads + kv_head) << a.page_shift) + (t & mask);
-            page = sqp_page(a, table, place(base + 64));
-            const uint8_t *kp = (const uint8_t *)a.k + r * (D * BYTES) + lane * 16;
+            for (int c = 0; c < NK; c++) qf[c] = *(const h16x8 *)(q + 16 * c);
+        };
+        // ---- staging; pages are looked up a tile ahead
+        uint32_t kw[4 * KL], vw[8 * VW];
+        float kscale = 0.f, kvscale = 0.f, vscale = 0.f;
+        bool bad = false;
+        auto place = [&](int base) { return min(base + 16 * block16, (hi - 1) & ~15); };
+        auto look_up = [&](int base) { return lo < hi ? sqp_page(a, table, place(base)) : 0; };
+        auto cache_row = [&](int page, int base) {
+            return (((size_t)__builtin_amdgcn_readfirstlane(page) * a.kv_heads + kv_head) << a.page_shift) + (place(base) & mask);
+        };
+        int page_k = look_up(lo), page_v = page_k;
+        auto load_k = [&](int base) {
+            const size_t r = cache_row(page_k, base) + first_token;
+            page_k = look_up(base + 64);
+            const uint8_t *kp = (const uint8_t *)a.k + r * (D * BYTES) + lane % (TOKENS * KU) * 16;
 #pragma unroll
-            for (int i = 0; i < KP; i++) kw[i] = *(const u32x4 *)(kp + 1024 * i);
-            const uint8_t *vp = (const uint8_t *)a.v + r * (D * BYTES) + 4 * h * (D * BYTES) + col * VB;
-#pragma unroll
-            for (int j = 0; j < 8; j++) sqp_words<VB>(vp + (8 * (j >> 2) + (j & 3)) * (D * BYTES), vw[j]);
-            if constexpr (TYPE != SQP_FP16) {
-                kscale = a.k_scales[r + (lane & 15)];
-                vscale = a.v_scales[r + (lane & 15)];
+            for (int i = 0; i < KL; i++) sqp_words<16>(kp + 1024 * i, &kw[4 * i]);
+            if constexpr (CODES) {
+                kscale = a.k_scales[r + lane % TOKENS];
+                kvscale = a.v_scales[r + lane % TOKENS];
             }
         };
-        bool bad = false;
-        auto store = [&](int base, int buf) {
-            if (base + 64 > least) {  // tokens that not all rows see, or that are none (memory past the length)
+        auto load_v = [&](int base) {
+            const size_t r = cache_row(page_v, base);
+            page_v = look_up(base + 64);
+            const uint8_t *vp = (const uint8_t *)a.v + (r + 4 * v_half) * (D * BYTES) + v_lane * VB;
+#pragma unroll
+            for (int j = 0; j < 8; j++) sqp_words<VB>(vp + (8 * (j >> 2) + (j & 3)) * (D * BYTES), &vw[j * VW]);
+            if constexpr (CODES) vscale = a.v_scales[r + first_token + lane % TOKENS];
+        };
+        // (The empty statements keep a piece's work, and with it the wait for its loads, where the piece is.)
+        auto store_k = [&](int buf, int piece) {
+            const int i = CODES ? piece / 2 : piece, unit = lane % (TOKENS * KU) + 64 * i;
+#pragma unroll
+            for (int e = 0; e < 4; e++) asm volatile("" : "+v"(kw[4 * i + e]));
+            h16 *to = &s_k[buf][(16 * block16 + first_token + unit / KU) * KROW];
+            if constexpr (CODES) {
+                h16x2 p[4];
+                sqp_halves4<TYPE>(kw[4 * i + 2 * (piece & 1)], p[0], p[1]);
+                sqp_halves4<TYPE>(kw[4 * i + 2 * (piece & 1) + 1], p[2], p[3]);
+                *(h16x8 *)&to[16 * (unit % KU) + 8 * (piece & 1)] = h16x8{p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
+                if (piece == KPIECES - 1 && lane < TOKENS) {
+                    s_ks[buf][16 * block16 + first_token + lane] = kscale * a.scale2;
+                    const float x = fmaxf(kvscale, 0x1p-100f);
+                    s_lv[buf][16 * block16 + first_token + lane] = kvscale == kvscale ? __builtin_amdgcn_logf(x) : kvscale;
+                }
+            } else {
+                *(u32x4 *)&to[8 * (unit % KU)] = u32x4{kw[4 * i], kw[4 * i + 1], kw[4 * i + 2], kw[4 * i + 3]};
+            }
+        };
+        // Tokens past the length (whatever memory holds there), and values that not all rows see and that are not finite.
+        auto inspect_v = [&](int base) {
+            if (__builtin_expect(base + 64 > least, 0)) {
 #pragma unroll
                 for (int j = 0; j < 8; j++) {
-                    const int key = base + 16 * wave + 8 * (j >> 2) + 4 * h + (j & 3);
+                    const int key = base + 16 * block16 + 8 * (j >> 2) + 4 * v_half + (j & 3);
 #pragma unroll
                     for (int e = 0; e < VW; e++) {
-                        if (key >= s.len) vw[j][e] = 0;
-                        else bad = bad || sqp_not_finite<TYPE>(vw[j][e]);
+                        if (key >= s.len) vw[j * VW + e] = 0;
+                        else bad = bad || sqp_not_finite<TYPE>(vw[j * VW + e]);
                     }
                 }
-                if constexpr (TYPE != SQP_FP16) {
-                    if (base + 16 * wave + (lane & 15) >= s.len) vscale = 0.f;
+                if constexpr (CODES) {
+                    if (base + 16 * block16 + first_token + lane % TOKENS >= s.len) vscale = 0.f;
                     bad = bad || !(__builtin_fabsf(vscale) < INFINITY);
                 }
             }
+        };
+        auto store_v = [&](int buf, int d) {
+            u32x4 x;
 #pragma unroll
-            for (int i = 0; i < KP; i++) {
-                const int unit = lane + 64 * i, key = 16 * wave + unit / KU, piece = unit % KU;
-                if constexpr (TYPE == SQP_FP16) {
-                    *(u32x4 *)&s_k[buf][key * D + 8 * (piece ^ (key & (D / 8 - 1)))] = kw[i];
+            for (int j = 0; j < 8; j++) asm volatile("" : "+v"(vw[j * VW + d * BYTES / 4]));
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[j] = sqp_pair<TYPE>(&vw[2 * j * VW], &vw[(2 * j + 1) * VW], d);
+            *(u32x4 *)&s_v[buf][(32 * VSUB * d + v_lane) * VROW + 16 * block16 + 8 * v_half] = x;
+            if (CODES && d == VD - 1 && lane < TOKENS) s_rv[buf][16 * block16 + first_token + lane] = 1.f / fmaxf(vscale, 0x1p-100f);
+        };
+
+        // ---- steps
+        float m = SQP_LOWEST, l = 0.f, l2 = 0.f, top = 0.f;  // l2: every second one's share of the sum
+        f32x16 o[NV], t, u;
+#pragma unroll
+        for (int d = 0; d < NV; d++) o[d] = (f32x16)(0.f);
+        h16x8 kf[AHEAD], vf[AHEAD], pf[2];
+        f32x4 ks[2], lv[2], rv[2];
+        auto fetch_k = [&](int buf, int half, int c) { kf[c % AHEAD] = *(const h16x8 *)&s_k[buf][(32 * half + col) * KROW + 16 * c + 8 * h]; };
+        auto fetch_v = [&](int buf, int half, int n) {
+            vf[n % AHEAD] = *(const h16x8 *)&s_v[buf][(32 * (n % NV) + col) * VROW + 32 * half + 16 * (n / NV) + 8 * h];
+        };
+        // result register r of a step's scores: token 8 (r >> 2) + 4 h + (r & 3) of its 32
+        auto fetch_ks = [&](int buf, int half, int r4) {
+            if constexpr (CODES) {
+                ks[r4 & 1] = *(const f32x4 *)&s_ks[buf][32 * half + 8 * r4 + 4 * h];
+                lv[r4 & 1] = *(const f32x4 *)&s_lv[buf][32 * half + 8 * r4 + 4 * h];
+            }
+        };
+        auto fetch_rv = [&](int buf, int half, int r4) {
+            if constexpr (CODES) rv[r4 & 1] = *(const f32x4 *)&s_rv[buf][32 * half + 8 * r4 + 4 * h];
+        };
+        // A fourth of a step's scores: their scales, and the row's largest (fp16: scores are scaled as p is formed).
+        auto take_max = [&](f32x16 &x, int r4) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                if constexpr (CODES) x[4 * r4 + e] = __builtin_fmaf(x[4 * r4 + e], ks[r4 & 1][e], lv[r4 & 1][e]);
+                top = r4 == 0 && e == 0 ? x[0] : fmaxf(top, x[4 * r4 + e]);
+            }
+            asm volatile("" : "+v"(top));
+        };
+        // p of result register n (8 of either 16 tokens) comes about in three stages, which the steps keep apart: one that follows
+        // the other at once would wait for it.
+        f32x16 e;
+        auto stage1 = [&](const f32x16 &x, int n) {
+            float v = CODES ? x[n] - m : __builtin_fmaf(x[n], a.scale2, -m);
+            asm volatile("" : "+v"(v));
+            e[n] = v;
+        };
+        auto stage2 = [&](int n) {
+            float p = sqp_exp2(e[n]);
+            asm volatile("" : "+v"(p));
+            e[n] = p;
+        };
+        auto stage3 = [&](int n) {  // two of them
+            const h16x2 p = {(h16)e[n], (h16)e[n + 1]};
+            pf[n >> 3][n & 7] = p.x;
+            pf[n >> 3][(n & 7) + 1] = p.y;
+            if constexpr (CODES) {
+                l = __builtin_fmaf(e[n], rv[n >> 2 & 1][n & 3], l);
+                l2 = __builtin_fmaf(e[n + 1], rv[n >> 2 & 1][(n & 3) + 1], l2);
+                asm volatile("" : "+v"(l2));
+            } else {
+                l = __builtin_amdgcn_fdot2(p, h16x2{(h16)1.f, (h16)1.f}, l, false);
+            }
+            asm volatile("" : "+v"(l));
+        };
+        // Masks and the running maximum, once a step's scores are there.  p stays below 2^15, inside fp16's range, with the
+        // maximum changed only now and then: at the first tokens, and where a score outgrows it by 2^15.
+        auto settle = [&](f32x16 &x, int base) {
+            if (__builtin_expect(base + 32 > wave_least, 0)) {
+                top = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    int left = sees - base - 4 * h;
+                    asm volatile("" : "+v"(left));  // (known to be the same sixteen times, the comparisons become one chain)
+                    x[r] = 8 * (r >> 2) + (r & 3) >= left ? -INFINITY : x[r];
+                    top = fmaxf(top, x[r]);
+                }
+            }
+            const float reach = CODES ? top : top * a.scale2;
+            if (__builtin_expect(__any(reach > m + 15.f), 0)) {
+                const float both = fmaxf(reach, __shfl_xor(reach, 32, 64)), next = both > m + 15.f ? both : m, keep = sqp_exp2(m - next);
+                m = next;
+                l *= keep;
+                l2 *= keep;
+#pragma unroll
+                for (int d = 0; d < NV; d++) o[d] *= keep;
+            }
+        };
+        // One step: the softmax and output of the scores x with V of (vbuf, vhalf), and the next step's scores y with K of
+        // (kbuf, khalf).  The matrix instructions are NK/2 of the scores, then the others in turn with the first 16
+        // tokens' output, then the last 16 tokens' output; pieces of the staged tile are stored beside the last ones.
+        auto step = [&](f32x16 &x, f32x16 &y, int vbuf, int vhalf, int kbuf, int khalf, int pieces, auto store) {
+            constexpr int MIXED = NK / 2 + NK / 2 + NV, ALL = NK + 2 * NV;
+#pragma unroll
+            for (int c = 0; c < AHEAD; c++) fetch_k(kbuf, khalf, c);
+#pragma unroll
+            for (int r4 = 0; r4 < 2; r4++) fetch_rv(vbuf, vhalf, r4);
+            y = (f32x16)(0.f);
+            __builtin_amdgcn_sched_barrier(0);
+            // stage 2 of how many p is done behind matrix instruction n: the first 8 before the first output asks for them, the other 8
+            // before the last 16 tokens'; stage 1 an instruction before, stage 3 one after
+            auto due = [](int n) {
+                return n < 0 ? 0 : n < NK / 2 ? (n + 1) * 8 / (NK / 2) : n < MIXED - 1 ? 8 + (n + 1 - NK / 2) * 8 / (MIXED - 1 - NK / 2) : 16;
+            };
+            int kn = 0, vn = 0, done1 = 0, done2 = 0, done3 = 0;
+#pragma unroll
+            for (; done1 < 8; done1++) stage1(x, done1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < ALL; n++) {
+                if (n < NK / 2 || (n < MIXED && (n - NK / 2) % 2 == 0)) {
+                    y = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[kn % AHEAD], qf[kn], y, 0, 0, 0);
+                    asm volatile("" : "+v"(y));  // (keeps the instruction here)
+                    if (kn < AHEAD) fetch_v(vbuf, vhalf, kn);
+                    if (kn + AHEAD < NK) fetch_k(kbuf, khalf, kn + AHEAD);
+                    kn++;
                 } else {
-                    const uint32_t w[4] = {kw[i].x, kw[i].y, kw[i].z, kw[i].w};
+                    o[vn % NV] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[vn % AHEAD], pf[vn / NV], o[vn % NV], 0, 0, 0);
+                    asm volatile("" : "+v"(o[vn % NV]));
+                    if (vn + AHEAD < 2 * NV) fetch_v(vbuf, vhalf, vn + AHEAD);
+                    vn++;
+                }
 #pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        h16x2 p[4];
-                        sqp_halves4<TYPE>(w[2 * e], p[0], p[1]);
-                        sqp_halves4<TYPE>(w[2 * e + 1], p[2], p[3]);
-                        const h16x8 x = {p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
-                        *(h16x8 *)&s_k[buf][key * D + 8 * ((2 * piece + e) ^ (key & (D / 8 - 1)))] = x;
+                for (; done1 < due(n + 1); done1++) stage1(x, done1);
+#pragma unroll
+                for (; done2 < due(n); done2++) stage2(done2);
+#pragma unroll
+                for (; done3 + 2 <= due(n - 1); done3 += 2) {
+                    stage3(done3);
+                    if (done3 % 4 == 2 && done3 < 8) fetch_rv(vbuf, vhalf, done3 / 4 + 2);
+                }
+                if (n >= MIXED - 2 && n < MIXED) fetch_ks(kbuf, khalf, n - (MIXED - 2));
+                if (n >= MIXED) {
+                    const int i = n - MIXED;  // of NV
+#pragma unroll
+                    for (int r4 = i * 4 / NV; r4 < (i + 1) * 4 / NV; r4++) {
+                        take_max(y, r4);
+                        if (r4 < 2) fetch_ks(kbuf, khalf, r4 + 2);
                     }
+#pragma unroll
+                    for (int piece = i * pieces / NV; piece < (i + 1) * pieces / NV; piece++) store(piece);
                 }
-            }
-            uint32_t pairs[4][VB < 4 ? 4 : VD];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-#pragma unroll
-                for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(vw[2 * j][e], vw[2 * j + 1][e], &pairs[j][e * (4 / BYTES)]);
-            }
-#pragma unroll
-            for (int d = 0; d < VD; d++) {
-                const int dim = VD * col + d;
-                const u32x4 x = {pairs[0][d], pairs[1][d], pairs[2][d], pairs[3][d]};
-                *(u32x4 *)&s_v[buf][dim * 64 + 8 * ((2 * wave + h) ^ ((dim ^ (dim >> 2)) & 7))] = x;
-            }
-            if constexpr (TYPE != SQP_FP16) {
-                float top = __builtin_fabsf(vscale);
-#pragma unroll
-                for (int off = 8; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-                if (lane < 16) {
-                    s_ks[buf][16 * wave + lane] = kscale * a.scale2;
-                    s_vs[buf][16 * wave + lane] = vscale;
-                }
-                if (lane == 0) s_lv[buf][wave] = ceilf(__builtin_amdgcn_logf(top));
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
 
-        float m = SQP_LOWEST, l = 0.f, lv = TYPE == SQP_FP16 ? 0.f : -60.f;
-        f32x16 o[D / 32];
-#pragma unroll
-        for (int d = 0; d < D / 32; d++) o[d] = (f32x16)(0.f);
         if (threadIdx.x == 0) s_bad = 0;
-        if (lo < hi) {
-            load(lo);
-            store(lo, 0);
+        if (lo < hi) {  // the first tile, and the second one's K; the third one's K and the second one's V are on their way then
+            load_k(lo);
+            load_v(lo);
+            load_q();
+            uint32_t first_kw[4 * KL];
+            const float first_kscale = kscale, first_kvscale = kvscale;
+#pragma unroll
+            for (int i = 0; i < 4 * KL; i++) first_kw[i] = kw[i];
+            load_k(lo + 64);
+            inspect_v(lo);
+#pragma unroll
+            for (int i = 0; i < VD; i++) store_v(0, i);
+            load_v(lo + 64);
+#pragma unroll
+            for (int i = 0; i < KPIECES; i++) store_k(1, i);
+#pragma unroll
+            for (int i = 0; i < 4 * KL; i++) kw[i] = first_kw[i];
+            kscale = first_kscale;
+            kvscale = first_kvscale;
+#pragma unroll
+            for (int i = 0; i < KPIECES; i++) store_k(0, i);
+            load_k(lo + 128);
+        } else {
+            load_q();
         }
-        // Q's loads end here: left to the loop, the wait for them would also be one for the next tile's loads, in every round.
+        // (Q's loads end here: left to the loop, the wait for them would also be one for the tiles' loads, in every round)
 #pragma unroll
-        for (int c = 0; c < D / 16; c++) asm volatile("" : "+v"(qf[c]));
-        int buf = 0;
-        for (int base = lo; base < hi; base += 64, buf ^= 1) {
-            __syncthreads();
-            const bool more = base + 64 < hi;
-            if (more) load(base + 64);
-            if (base < wave_most) {
-                // The order of instructions is fixed: the compiler's own waits for every operand as soon as it is asked for.
-                // Operands are fetched four matrix instructions ahead, and what has to be done to the first 32 tokens' scores is
-                // done beside the next 32's products.
-                f32x16 t[2];
-                t[0] = t[1] = (f32x16)(0.f);
-                h16x8 kf[AHEAD];
-                f32x4 ks[4];
-                auto fetch_k = [&](int n) {
-                    const int key = 32 * (n / (D / 16)) + col, c = n % (D / 16);
-                    kf[n % AHEAD] = *(const h16x8 *)&s_k[buf][key * D + 8 * ((2 * c + h) ^ (key & (D / 8 - 1)))];
-                };
-                // result register r of block i: token base + 32 i + 8 (r >> 2) + 4 h + (r & 3)
-                auto fetch_ks = [&](int i, int r4) { ks[r4] = *(const f32x4 *)&s_ks[buf][32 * i + 8 * r4 + 4 * h]; };
-                auto scale = [&](int i, int r4) {
+        for (int c = 0; c < NK; c++) asm volatile("" : "+v"(qf[c]));
+        __syncthreads();
+        if (lo < wave_most && lo < hi) {
+            t = (f32x16)(0.f);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) t[i][4 * r4 + e] *= ks[r4][e];
-                };
-#pragma unroll
-                for (int n = 0; n < AHEAD; n++) fetch_k(n);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int n = 0; n < D / 8; n++) {
-                    t[n / (D / 16)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[n % AHEAD], qf[n % (D / 16)], t[n / (D / 16)], 0, 0, 0);
-                    if (n + AHEAD < D / 8) fetch_k(n + AHEAD);
-                    if constexpr (TYPE != SQP_FP16) {  // (fp16: scores are scaled as p is formed)
-                        const int j = n - D / 16;
-                        if (j >= 0 && j < 4) fetch_ks(0, j);
-                        if (j == D / 16 - 1) {
-#pragma unroll
-                            for (int r4 = 0; r4 < 4; r4++) {
-                                scale(0, r4);
-                                fetch_ks(1, r4);
-                            }
-                        }
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                if constexpr (TYPE != SQP_FP16) {
-#pragma unroll
-                    for (int r4 = 0; r4 < 4; r4++) scale(1, r4);
-                }
-                if (base + 64 > wave_least) {
-#pragma unroll
-                    for (int i = 0; i < 2; i++)
-#pragma unroll
-                        for (int r = 0; r < 16; r++)
-                            if (base + 32 * i + 8 * (r >> 2) + 4 * h + (r & 3) >= sees) t[i][r] = -INFINITY;
-                }
-                float top = t[0][0];
-#pragma unroll
-                for (int r = 1; r < 32; r++) top = fmaxf(top, t[r >> 4][r & 15]);
-                if constexpr (TYPE == SQP_FP16) top *= a.scale2;
-                float tile_lv = lv;
-                if constexpr (TYPE != SQP_FP16) {
-                    const f32x4 x = *(const f32x4 *)s_lv[buf];
-                    tile_lv = fmaxf(lv, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-                }
-                // as in the few-rows kernel: p 2^-lv times a value's scale inside fp16's range
-                if (__any(top + tile_lv > m + 12.f)) {
-                    top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    const float next = top + tile_lv > m + 12.f ? top + tile_lv - 4.f : m, keep = sqp_exp2(m - next);
-                    m = next;
-                    l *= keep;
-#pragma unroll
-                    for (int d = 0; d < D / 32; d++) o[d] *= keep;
-                }
-                lv = tile_lv;
-                // p of step c + 1 is formed beside the matrix instructions of step c
-                h16x8 pf[2], vf[AHEAD];
-                f32x4 vs[2];
-                auto fetch_v = [&](int n) {
-                    const int c = n / (D / 32), dim = 32 * (n % (D / 32)) + col;
-                    vf[n % AHEAD] = *(const h16x8 *)&s_v[buf][dim * 64 + 8 * ((2 * c + h) ^ ((dim ^ (dim >> 2)) & 7))];
-                };
-                auto fetch_vs = [&](int c) {
-                    if constexpr (TYPE != SQP_FP16) {
-                        vs[0] = *(const f32x4 *)&s_vs[buf][16 * c + 4 * h];
-                        vs[1] = *(const f32x4 *)&s_vs[buf][16 * c + 8 + 4 * h];
-                    }
-                };
-                auto form = [&](int c, int from, int to) {
-#pragma unroll
-                    for (int j = from; j < to; j++) {
-                        const float x = t[c >> 1][8 * (c & 1) + j];
-                        const float p = sqp_exp2(TYPE == SQP_FP16 ? __builtin_fmaf(x, a.scale2, -m) : x - m);
-                        l += p;
-                        pf[c & 1][j] = (h16)(TYPE == SQP_FP16 ? p : p * vs[j >> 2][j & 3]);
-                    }
-                };
-                fetch_vs(0);
-#pragma unroll
-                for (int n = 0; n < AHEAD; n++) fetch_v(n);
-                __builtin_amdgcn_sched_barrier(0);
-                form(0, 0, 8);
-                fetch_vs(1);
-                __builtin_amdgcn_sched_barrier(0);
-                constexpr int ND = D / 32, SHARE = 8 / ND;
-#pragma unroll
-                for (int n = 0; n < 4 * ND; n++) {
-                    const int c = n / ND, d = n % ND;
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[n % AHEAD], pf[c & 1], o[d], 0, 0, 0);
-                    if (n + AHEAD < 4 * ND) fetch_v(n + AHEAD);
-                    if (c < 3) form(c + 1, SHARE * d, SHARE * (d + 1));
-                    if (c < 2 && d == ND - 1) fetch_vs(c + 2);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            for (int c = 0; c < NK; c++) {
+                fetch_k(0, 0, c);
+                t = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[c % AHEAD], qf[c], t, 0, 0, 0);
             }
-            if (more) store(base + 64, buf ^ 1);
+#pragma unroll
+            for (int r4 = 0; r4 < 4; r4++) {
+                fetch_ks(0, 0, r4);
+                take_max(t, r4);
+            }
+            settle(t, lo);
         }
+        int kbuf = 0, vbuf = 0;
+        for (int base = lo; base < hi; base += 64) {
+            const int vnext = vbuf == VBUFS - 1 ? 0 : vbuf + 1;
+            const bool active = base < wave_most;
+            inspect_v(base + 64);
+            auto keep_v = [&](int i) { store_v(vnext, i); };
+            if (active) {
+                step(t, u, vbuf, 0, kbuf, 1, VD, keep_v);
+                settle(u, base + 32);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VD; i++) keep_v(i);
+            }
+            load_v(base + 128);
+            __syncthreads();
+            auto keep_k = [&](int i) { store_k(kbuf, i); };
+            if (active) {
+                step(u, t, vbuf, 1, kbuf ^ 1, 0, KPIECES, keep_k);
+                settle(t, base + 64);
+            } else {
+#pragma unroll
+                for (int i = 0; i < KPIECES; i++) keep_k(i);
+            }
+            load_k(base + 192);
+            if (VBUFS == 2) __syncthreads();
+            kbuf ^= 1;
+            vbuf = vnext;
+        }
+        l += l2;
         l += __shfl_xor(l, 32, 64);
         if (bad) s_bad = 1;
         __syncthreads();
         if (s_bad) {
-            for (int r = row0 + wave; r <= row_last; r += 4) {
+            for (int r = row0 + wave; r <= row_last; r += W) {
                 const int tk = r / a.group;
                 sqp_attend_row_of_part<TYPE, D>(a, parts, part, s.first + tk, kv_head * a.group + r - tk * a.group, before + tk + 1, table, lo, hi);
             }
@@ -277,20 +378,26 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
             float *partial;
             if (sqp_target<D>(parts, sees, part, at, partial)) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
+                // result register r of block VSUB d + sub: dimension VD (32 sub + i) + d, i = 8 (r >> 2) + 4 h + (r & 3)
 #pragma unroll
-                for (int d = 0; d < D / 32; d++)
+                for (int sub = 0; sub < VSUB; sub++)
 #pragma unroll
-                    for (int r4 = 0; r4 < 4; r4++) {
-                        const int dim = 32 * d + 8 * r4 + 4 * h;
-                        if (partial) {
-                            *(f32x4 *)(partial + dim) = f32x4{o[d][4 * r4], o[d][4 * r4 + 1], o[d][4 * r4 + 2], o[d][4 * r4 + 3]};
-                        } else {
-                            h16x4 y;
+                    for (int r4 = 0; r4 < 4; r4++)
 #pragma unroll
-                            for (int e = 0; e < 4; e++) y[e] = (h16)(l == 0.f ? 0.f : o[d][4 * r4 + e] * inv);
-                            *(h16x4 *)(a.out + at * D + dim) = y;
+                        for (int n = 0; n < VD; n++) {
+                            const int dim = VD * (32 * sub + 8 * r4 + 4 * h) + 4 * n;
+                            f32x4 x;
+#pragma unroll
+                            for (int e = 0; e < 4; e++) x[e] = o[VSUB * ((4 * n + e) % VD) + sub][4 * r4 + (4 * n + e) / VD];
+                            if (partial) {
+                                *(f32x4 *)(partial + dim) = x;
+                            } else {
+                                h16x4 y;
+#pragma unroll
+                                for (int e = 0; e < 4; e++) y[e] = (h16)(l == 0.f ? 0.f : x[e] * inv);
+                                *(h16x4 *)(a.out + at * D + dim) = y;
+                            }
                         }
-                    }
                 if (partial && h == 0) {
                     partial[D] = m;
                     partial[D + 1] = l;
@@ -301,19 +408,26 @@ __global__ void __launch_bounds__(256, 2) attention_tiles_kernel(const SqpAttent
     }
 }
 
-template <int TYPE, int D>
-void launch(const SqpAttention &a, const SqpParts &p, int above_rows, int max_q, hipStream_t st)
+template <int TYPE, int D, int W>
+void launch(const SqpAttention &a, const SqpParts &p, int above_rows, int fold, hipStream_t st)
 {
-    const long rows = (long)max_q * a.group;
-    const long tiles = std::min((rows + SQP_TILE_ROWS - 1) / SQP_TILE_ROWS, 65535L / p.parts);
-    attention_tiles_kernel<TYPE, D><<<dim3((unsigned)a.kv_heads, (unsigned)(tiles * p.parts), (unsigned)a.B), 256, 0, st>>>(a, p, above_rows, (int)tiles);
+    // every sequence may end inside a tile
+    const long tiles = std::min((long)a.T * a.group / (32 * W) + a.B, 65535L / p.parts);
+    attention_tiles_kernel<TYPE, D, W><<<dim3((unsigned)a.kv_heads, (unsigned)(tiles * p.parts)), 64 * W, 0, st>>>(a, p, above_rows, fold);
+}
+
+template <int TYPE, int D>
+void launch(const SqpAttention &a, const SqpParts &p, int tile_rows, int above_rows, int fold, hipStream_t st)
+{
+    if (tile_rows == 256) launch<TYPE, D, 8>(a, p, above_rows, fold, st);
+    else launch<TYPE, D, 4>(a, p, above_rows, fold, st);
 }
 
 }  // namespace
 
-void sqp_attention_tiles(int type, int D, const SqpAttention &a, const SqpParts &p, int above_rows, int max_q, hipStream_t st)
+void sqp_attention_tiles(int type, int D, const SqpAttention &a, const SqpParts &p, int tile_rows, int above_rows, int fold, hipStream_t st)
 {
-#define TILES(TYPE) (D == 128 ? launch<TYPE, 128>(a, p, above_rows, max_q, st) : launch<TYPE, 64>(a, p, above_rows, max_q, st))
+#define TILES(TYPE) (D == 128 ? launch<TYPE, 128>(a, p, tile_rows, above_rows, fold, st) : launch<TYPE, 64>(a, p, tile_rows, above_rows, fold, st))
     if (type == SQP_FP16) TILES(SQP_FP16);
     else if (type == SQP_INT8) TILES(SQP_INT8);
     else TILES(SQP_E4M3);
