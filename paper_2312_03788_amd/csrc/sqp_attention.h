@@ -119,6 +119,9 @@ __device__ __forceinline__ bool sqp_not_finite(uint32_t w)
     return false;
 }
 
+// An index array's element at the same place for a whole wave, through the scalar cache (no kernel writes these arrays).
+__device__ __forceinline__ int sqp_uniform(const int *p) { return *(const __attribute__((address_space(4))) int *)(uintptr_t)p; }
+
 // The new tokens of a sequence, its length in the cache.  What the device arrays say is kept inside the tensors.
 struct SqpSequence {
     int first, n, len;
@@ -133,6 +136,20 @@ __device__ __forceinline__ SqpSequence sqp_sequence(const SqpAttention &a, int b
         s.n = max(min(a.starts[b + 1], a.T) - s.first, 0);
     }
     s.len = min(max(a.lens[b], 0), a.table_width << a.page_shift);
+    return s;
+}
+
+// The same where b is the same for the whole wave.
+__device__ __forceinline__ SqpSequence sqp_one_sequence(const SqpAttention &a, int b)
+{
+    SqpSequence s;
+    s.first = b;
+    s.n = 1;
+    if (a.starts) {
+        s.first = min(max(sqp_uniform(a.starts + b), 0), a.T);
+        s.n = max(min(sqp_uniform(a.starts + b + 1), a.T) - s.first, 0);
+    }
+    s.len = min(max(sqp_uniform(a.lens + b), 0), a.table_width << a.page_shift);
     return s;
 }
 

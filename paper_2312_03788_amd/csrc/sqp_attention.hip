@@ -15,30 +15,36 @@ template <int D>
 __global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttention a, const SqpParts few, const SqpParts tiles, int most_rows)
 {
     constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 6);  // (T heads D < 2^31)
+    const int row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));  // (T heads D < 2^31)
     if (row >= a.T * a.heads) return;
-    const int lane = threadIdx.x & 63, token = __builtin_amdgcn_readfirstlane(row / a.heads);
+    const int lane = threadIdx.x & 63, token = row / a.heads, d = 4 * (lane % LANES), which = lane / LANES;
+    // read before it is known how many parts there are: the chain of loads is what this kernel takes
+    const int pitch = few.pitch;
+    const float *part = few.part + (size_t)row * pitch * (D + 4);
+    const float m0 = part[min(lane, pitch - 1) * (D + 4) + D], l0 = part[min(lane, pitch - 1) * (D + 4) + D + 1];
+    f32x4 x[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) x[j] = *(const f32x4 *)&part[min(j * AT_ONCE + which, pitch - 1) * (D + 4) + d];
     const int b = __builtin_amdgcn_readfirstlane(sqp_sequence_of(a, token));
     if (b >= a.B) return;
-    const SqpSequence s = sqp_sequence(a, b);
+    const SqpSequence s = sqp_one_sequence(a, b);
     const SqpParts &p = s.n * a.group <= most_rows ? few : tiles;
     const int n = p.of(s.len - s.n + (token - s.first) + 1);
     if (n == 1) return;
-    const float *part = p.part + (size_t)row * p.pitch * (D + 4);
-    const float m = lane < n ? part[lane * (D + 4) + D] : SQP_LOWEST;
+    const float m = lane < n ? m0 : SQP_LOWEST;
     float top = m;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    const float w = lane < n ? sqp_exp2(m - top) : 0.f;  // (no weight past the last part)
-    float sum = lane < n ? w * part[lane * (D + 4) + D + 1] : 0.f;
+    const float w = lane < n ? sqp_exp2(m - top) : 0.f;
+    float sum = lane < n ? w * l0 : 0.f;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    const int d = 4 * (lane % LANES), which = lane / LANES;
     f32x4 o = (f32x4)(0.f);
     for (int i = 0; i < n; i += 4 * AT_ONCE) {
-        f32x4 x[4];
+        if (i > 0) {
 #pragma unroll
-        for (int j = 0; j < 4; j++) x[j] = *(const f32x4 *)&part[min(i + j * AT_ONCE + which, n - 1) * (D + 4) + d];
+            for (int j = 0; j < 4; j++) x[j] = *(const f32x4 *)&part[min(i + j * AT_ONCE + which, n - 1) * (D + 4) + d];
+        }
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             const int at = i + j * AT_ONCE + which;

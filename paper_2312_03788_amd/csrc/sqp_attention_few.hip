@@ -1,7 +1,7 @@
 // Attention over the paged cache for few rows per cached head: decode steps, a few tokens at a time.  Bound: the bytes of the
 // cache.
 //
-// Four waves of a workgroup share a (sequence, cached head, part) and take 32 tokens of it in turn; nothing passes between them
+// Four waves of a workgroup share a (sequence, cached head, part) and take 32 (codes: 64) tokens of it in turn; nothing passes between them
 // before the end.  Both products run on 16x16x32 matrix instructions with the up to 16 query rows as columns:
 //   S^T = K Q^T   a lane's A operand is 8 values of one key, as they lie in memory (a lane's 16-byte loads: 16 keys x 64 bytes);
 //                 the values' order within D is free as long as Q has the same.
@@ -21,19 +21,21 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
     constexpr int KL = D * BYTES / 64;       // 16-byte loads per lane and 16 keys
     constexpr int VW = D * BYTES / 64;       // words per lane and token of V
     constexpr int DPL = D / 16;              // dimensions per lane of V
+    constexpr int NB = TYPE == SQP_FP16 ? 2 : 4;  // blocks of 16 tokens per step: codes are half as long, so twice as many keep
+                                                  // the same number of bytes on their way
     __shared__ float s_o[4][SQP_FEW_ROWS][D + 4];
     __shared__ float s_m[4][SQP_FEW_ROWS], s_l[4][SQP_FEW_ROWS];
     __shared__ int s_bad;
 
     const int kv_head = blockIdx.x, b = blockIdx.y, part = blockIdx.z;
     if (part == 0 && b == 0) sqp_zero_strays<D>(a, kv_head);
-    const SqpSequence s = sqp_sequence(a, b);
+    const SqpSequence s = sqp_one_sequence(a, b);
     const int rows = s.n * a.group;
     if (rows > most_rows) return;
     const int *table = a.table + b * a.table_stride;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
     const int before = s.len - s.n;  // token i of the new ones sees before + i + 1
-    const int mask = (1 << a.page_shift) - 1;
+    const int mask = (1 << a.page_shift) - 1, reach = a.table_width << a.page_shift;
     for (int row0 = 0; row0 < rows; row0 += SQP_FEW_ROWS) {  // (once, unless this kernel serves sequences of more rows)
         const int count = min(rows - row0, SQP_FEW_ROWS), fewest = before + row0 / a.group + 1, most = before + (row0 + count - 1) / a.group + 1;
         const int nparts = parts.of(most);
@@ -49,30 +51,33 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
 #pragma unroll
             for (int i = 0; i < D / 32; i++) qf[i] = *(const h16x8 *)(q + (BYTES == 2 ? 32 * i + 8 * g : 64 * (i >> 1) + 16 * g + 8 * (i & 1)));
         }
-        // Row in the caches of a 16-token block's first token (pages are whole blocks, so all 16 rows are there; a block that
-        // begins past the end reads the last one's).
-        auto block = [&](int t0) {
-            const int t = min(t0, (hi - 1) & ~15);
-            const size_t page = (size_t)sqp_page(a, table, t) * a.kv_heads + kv_head;
-            return (page << a.page_shift) + (t & mask);
-        };
-        u32x4 kw[2][KL];
-        uint32_t vw[8][VW];
-        f32x4 ks[2], vs[2];
-        auto load_k = [&](int base) {
+        // Rows in the caches of a step's blocks of 16 tokens (pages are whole blocks, so all 16 rows are there).  A block past the
+        // end is whatever the table has there, kept inside the cache.  Pages are looked up a step ahead.
+        auto look_up = [&](int base, int *page) {
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const size_t r = block(base + 16 * i);
+            for (int i = 0; i < NB; i++) page[i] = sqp_uniform(table + (min(base + 16 * i, reach - 16) >> a.page_shift));
+        };
+        auto block = [&](int base, int i, const int *page) {
+            const size_t at = (size_t)min(max(page[i], 0), a.pages - 1) * a.kv_heads + kv_head;
+            return (at << a.page_shift) + ((base + 16 * i) & mask);
+        };
+        u32x4 kw[NB][KL];
+        uint32_t vw[4 * NB][VW];
+        f32x4 ks[NB], vs[NB];
+        auto load_k = [&](int base, const int *page) {
+#pragma unroll
+            for (int i = 0; i < NB; i++) {
+                const size_t r = block(base, i, page);
                 const uint8_t *p = (const uint8_t *)a.k + r * (D * BYTES) + col * (D * BYTES) + 16 * g;
 #pragma unroll
                 for (int j = 0; j < KL; j++) kw[i][j] = *(const u32x4 *)(p + 64 * j);
                 if constexpr (TYPE != SQP_FP16) ks[i] = *(const f32x4 *)(a.k_scales + r + 4 * g);
             }
         };
-        auto load_v = [&](int base) {
+        auto load_v = [&](int base, const int *page) {
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const size_t r = block(base + 16 * i);
+            for (int i = 0; i < NB; i++) {
+                const size_t r = block(base, i, page);
                 const uint8_t *p = (const uint8_t *)a.v + r * (D * BYTES) + col * (DPL * BYTES);
 #pragma unroll
                 for (int j = 0; j < 4; j++) sqp_words<4 * VW>(p + (4 * g + j) * (D * BYTES), vw[4 * i + j]);
@@ -85,15 +90,18 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
 #pragma unroll
         for (int t = 0; t < DPL; t++) o[t] = (f32x4)(0.f);
         bool bad = false;
-        int base = lo + 32 * wave;
+        int base = lo + 16 * NB * wave;
+        int page[NB], ahead[NB];
+        look_up(base, page);
         if (base < hi) {
-            load_k(base);
-            load_v(base);
+            load_k(base, page);
+            load_v(base, page);
+            look_up(base + 64 * NB, page);
         }
-        for (; base < hi; base += 128) {
-            float t[8];
+        for (; base < hi; base += 64 * NB) {
+            float t[4 * NB];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
+            for (int i = 0; i < NB; i++) {
                 f32x4 acc = (f32x4)(0.f);
 #pragma unroll
                 for (int j = 0; j < KL; j++) {
@@ -114,12 +122,13 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
 #pragma unroll
                 for (int r = 0; r < 4; r++) t[4 * i + r] = TYPE == SQP_FP16 ? acc[r] * a.scale2 : acc[r] * (ks[i][r] * a.scale2);
             }
-            const bool more = base + 128 < hi;
-            if (more) load_k(base + 128);
+            const bool more = base + 64 * NB < hi;
+            look_up(base + 128 * NB, ahead);
+            if (more) load_k(base + 64 * NB, page);
             float vmax = 0.f;
-            if (base + 32 > fewest) {  // some row does not see all of these tokens
+            if (base + 16 * NB > fewest) {  // some row does not see all of these tokens
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
+                for (int i = 0; i < 4 * NB; i++) {
                     const int key = base + 16 * (i >> 2) + 4 * g + (i & 3);
                     if (key >= sees) t[i] = -INFINITY;
                     if (key >= s.len) {  // memory past the length, whatever it holds
@@ -136,12 +145,12 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             }
             float top = t[0];
 #pragma unroll
-            for (int i = 1; i < 8; i++) top = fmaxf(top, t[i]);
+            for (int i = 1; i < 4 * NB; i++) top = fmaxf(top, t[i]);
             if constexpr (TYPE != SQP_FP16) {
 #pragma unroll
-                for (int i = 0; i < 8; i++) vmax = fmaxf(vmax, __builtin_fabsf(vs[i >> 2][i & 3]));
+                for (int i = 0; i < 4 * NB; i++) vmax = fmaxf(vmax, __builtin_fabsf(vs[i >> 2][i & 3]));
             }
-            // p 2^-lv times a value's scale stays below 2^12 and the largest above 2^-5: inside fp16's range, with the running
+            // p 2^-lv times a value's scale stays below 2^15: inside fp16's range, with the running
             // maximum (in which lv, the logarithm of the largest scale, is counted) changed only now and then.
             if (__any(top + lv > m + 15.f || (TYPE != SQP_FP16 && vmax > sqp_exp2(lv)))) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -157,25 +166,29 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
 #pragma unroll
                 for (int d = 0; d < DPL; d++) o[d] *= keep;
             }
-            h16x8 pf;
+            h16x8 pf[NB / 2];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
+            for (int i = 0; i < 4 * NB; i++) {
                 const float p = sqp_exp2(t[i] - m);
                 l += p;
-                pf[i] = (h16)(TYPE == SQP_FP16 ? p : p * vs[i >> 2][i & 3]);
+                pf[i >> 3][i & 7] = (h16)(TYPE == SQP_FP16 ? p : p * vs[i >> 2][i & 3]);
             }
-            uint32_t pairs[4][DPL];  // [pair of tokens][dimension]
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
+            for (int q = 0; q < NB / 2; q++) {
+                uint32_t pairs[4][DPL];  // [pair of tokens][dimension]
 #pragma unroll
-                for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(vw[2 * j][e], vw[2 * j + 1][e], &pairs[j][e * (4 / BYTES)]);
+                for (int j = 0; j < 4; j++)
+#pragma unroll
+                    for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(vw[8 * q + 2 * j][e], vw[8 * q + 2 * j + 1][e], &pairs[j][e * (4 / BYTES)]);
+                if (more && q == NB / 2 - 1) load_v(base + 64 * NB, page);
+#pragma unroll
+                for (int d = 0; d < DPL; d++) {
+                    const u32x4 x = {pairs[0][d], pairs[1][d], pairs[2][d], pairs[3][d]};
+                    o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, x), pf[q], o[d], 0, 0, 0);
+                }
             }
-            if (more) load_v(base + 128);
 #pragma unroll
-            for (int d = 0; d < DPL; d++) {
-                const u32x4 x = {pairs[0][d], pairs[1][d], pairs[2][d], pairs[3][d]};
-                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, x), pf, o[d], 0, 0, 0);
-            }
+            for (int i = 0; i < NB; i++) page[i] = ahead[i];
         }
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);

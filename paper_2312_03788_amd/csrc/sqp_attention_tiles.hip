@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         const SqpTile at_tile = sqp_pick_tile(a, above_rows, ROWS, rank, fold);
         const int b = __builtin_amdgcn_readfirstlane(at_tile.b), tile = __builtin_amdgcn_readfirstlane(at_tile.tile);
         if (b < 0) break;
-        const SqpSequence s = sqp_sequence(a, b);
+        const SqpSequence s = sqp_one_sequence(a, b);
         const int rows = s.n * a.group;
         const int *table = a.table + b * a.table_stride;
         const int before = s.len - s.n;  // token i of the new ones sees before + i + 1
