@@ -453,8 +453,9 @@ _TYPES = {torch.float16: 0, torch.int8: 1, torch.float8_e4m3fn: 2}  # SQP_FP16, 
 
 def add_rmsnorm(x, residual, gamma, eps, out=None, sum_out=None):
     """(y, r): the new residual r = x + residual and its RMS norm y, both fp16 [M,H].  sum_out may be x or residual."""
-    if _native(x):
-        o = _fast.add_rmsnorm(0, x, residual, gamma, eps, out, sum_out, *_here())
+    if _fast is not None and isinstance(x, _Tensor) and x.is_cuda:  # (written out, here and below: calls cost 0.1 us each)
+        dev = _current_device()
+        o = _fast.add_rmsnorm(0, x, residual, gamma, eps, out, sum_out, dev, _raw_stream(dev))
         if o is not None:
             return o if type(o) is not int else _ended(o, "sqp_add_rmsnorm")
     M, H = x.shape
@@ -473,8 +474,9 @@ def add_rmsnorm_quant(x, residual, gamma, eps, dtype=torch.float8_e4m3fn, out=No
     """(codes, scales, r): add_rmsnorm with y in 8 bits (torch.int8 or torch.float8_e4m3fn [M,H]) and an fp32 scale per
     row [M].  out: (codes, scales)."""
     kind = _TYPES.get(dtype, 0)
-    if kind and out is None and _native(x):
-        o = _fast.add_rmsnorm(kind, x, residual, gamma, eps, None, sum_out, *_here())
+    if kind and out is None and _fast is not None and isinstance(x, _Tensor) and x.is_cuda:
+        dev = _current_device()
+        o = _fast.add_rmsnorm(kind, x, residual, gamma, eps, None, sum_out, dev, _raw_stream(dev))
         if o is not None:
             return o if type(o) is not int else _ended(o, "sqp_add_rmsnorm_quant")
     if not kind:
@@ -538,8 +540,9 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, k_scales=None, v_scales=None, 
     cache: not written) of the cache [pages, kv_heads, page, D] (fp16, or int8 / e4m3 with scales [pages, kv_heads, page]).
     With cos_sin [positions, D] fp32 and positions int32 [T], keys and q are rotated; returns the queries [T, heads, D], or None
     without q.  q, k and v may be views of a merged projection."""
-    if _native(k):
-        o = _fast.kv_cache_write(k, v, slots, k_cache, v_cache, k_scales, v_scales, q, cos_sin, positions, out, *_here())
+    if _fast is not None and isinstance(k, _Tensor) and k.is_cuda:
+        dev = _current_device()
+        o = _fast.kv_cache_write(k, v, slots, k_cache, v_cache, k_scales, v_scales, q, cos_sin, positions, out, dev, _raw_stream(dev))
         if o is not None:
             return (None if o is True else o) if type(o) is not int else _ended(o, "sqp_kv_cache_write")
     (pages, kv_heads, page, D, kind), cache = _cache(k_cache, v_cache, k_scales, v_scales)
@@ -571,8 +574,9 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, k_scales=None, v_scales=None, 
 
 def kv_cache_read(slots, k_cache, v_cache, k_scales=None, v_scales=None, out=None):
     """(k, v): the slots' keys and values as fp16 [T, kv_heads, D] (zeros for slots outside the cache).  out: (k, v)."""
-    if out is None and _native(slots):
-        o = _fast.kv_cache_read(slots, k_cache, v_cache, k_scales, v_scales, *_here())
+    if out is None and _fast is not None and isinstance(slots, _Tensor) and slots.is_cuda:
+        dev = _current_device()
+        o = _fast.kv_cache_read(slots, k_cache, v_cache, k_scales, v_scales, dev, _raw_stream(dev))
         if o is not None:
             return o if type(o) is not int else _ended(o, "sqp_kv_cache_read")
     (pages, kv_heads, page, D, kind), cache = _cache(k_cache, v_cache, k_scales, v_scales)
@@ -596,8 +600,9 @@ def paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts=None, k_
     ones among them), q_starts int32 [B + 1] (None: one new token per sequence).  max_q, max_len: the most new tokens and the
     greatest length, if the caller knows them (the work is laid out by them; larger ones are right, only slower).  scale: of the
     scores, D^-0.5 by default."""
-    if _native(q):
-        o = _fast.paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts, k_scales, v_scales, max_q, max_len, scale, out, *_here())
+    if _fast is not None and isinstance(q, _Tensor) and q.is_cuda:
+        dev = _current_device()
+        o = _fast.paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts, k_scales, v_scales, max_q, max_len, scale, out, dev, _raw_stream(dev))
         if o is not None:
             return o if type(o) is not int else _ended(o, "sqp_paged_attention")
     (pages, kv_heads, page, D, kind), cache = _cache(k_cache, v_cache, k_scales, v_scales)

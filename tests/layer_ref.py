@@ -112,8 +112,8 @@ class Step:
         x = cache.view(torch.uint8)[pages, :, place].view(cache.dtype) if cache.dtype == torch.float8_e4m3fn else cache[pages, :, place]
         return dequantised(x, None if scales is None else scales[pages, :, place]).transpose(0, 1)
 
-    def expected(self, scale=None):
-        """(out, tolerance) [T, heads, D] in 64 bits.
+    def expected(self, scale=None, rows=None):
+        """(out, tolerance) [T, heads, D] in 64 bits (rows: (sequence, new token, head) to compute, the others are left zero).
 
         The kernels hold scores, sums and outputs in fp32 and round p to fp16 once, the output once.  With A = sum_j p_j |v_j|:
           output's rounding       2^-11 |o| + 2^-25 (half a step, half of the smallest one)
@@ -132,8 +132,10 @@ class Step:
             k, v = self.rows(b, self.k, self.ks), self.rows(b, self.v, self.vs)
             sees = torch.arange(length)[None, :] <= (length - n + torch.arange(n))[:, None]
             for h in range(self.heads):
+                if rows is not None and not any(r[0] == b and r[2] == h for r in rows):
+                    continue
                 q, kh, vh = self.q[first: first + n, h].double(), k[h // group], v[h // group]
-                for i in range(n):  # (one row at a time over what it sees: what it does not see may be NaN)
+                for i in range(n) if rows is None else [r[1] for r in rows if r[0] == b and r[2] == h]:  # (one row at a time over what it sees: what it does not see may be NaN)
                     m = int(sees[i].sum())
                     if m == 0:
                         continue

@@ -272,6 +272,55 @@ def test_attention(sqp, case, kind):
         assert torch.equal(got, sqp.paged_attention(**a, max_q=1, max_len=max(lens)))
 
 
+@pytest.mark.parametrize("kind", ["fp16", "int8", "e4m3"])
+@pytest.mark.parametrize("heads,kv,D,lens,news", [
+    (32, 32, 64, [4096], [4096]),                       # as many tiles as take the 256-row form, one sequence
+    (64, 8, 128, [2300, 1500], [1100, 1029]),           # and two
+    (64, 16, 128, [600, 2111, 33, 700], [600, 1, 33, 500]),
+    (8, 8, 128, [1025], [1025])])
+def test_attention_many_rows(sqp, heads, kv, D, lens, news, kind):
+    """Long prompts: sampled rows (the first and last of every tile edge's neighbourhood among them) of sampled heads."""
+    print("case many rows", heads, kv, D, lens, news, kind, flush=True)
+    step = ref.Step(lens, news, heads, kv, D, 64, kind, seed=30)
+    got = sqp.paged_attention(**step.gpu(), max_q=max(news), max_len=max(lens)).cpu()
+    assert bool(got.isfinite().all())
+    rows = [(b, i, h) for b, n in enumerate(news) for i in sorted({0, 1, n // 3, n // 2, n - 2, n - 1, *range(31, n, max(32, n // 8)), *range(32, n, max(32, n // 8))})
+            if 0 <= i < n for h in (0, heads // 2 + 1, heads - 1)]
+    want, tol = step.expected(rows=rows)
+    at = [(int(step.starts[b]) + i, h) for b, i, h in rows]
+    t, h = torch.tensor([a[0] for a in at]), torch.tensor([a[1] for a in at])
+    err = (got[t, h].double() - want[t, h]).abs()
+    assert bool((err <= tol[t, h]).all()), "worst error / tolerance %.3f" % float((err / tol[t, h]).max())
+
+
+@pytest.mark.parametrize("kind", ["fp16", "int8"])
+def test_attention_many_rows_later_token_not_a_number(sqp, kind):
+    """The slow way of the 256-row form."""
+    step = ref.Step([900], [900], 160, 160, 64, 16, kind, seed=31)
+    free = torch.zeros((step.k.shape[0], 16), dtype=torch.bool)
+    free[step.table[0, 899 // 16].long(), 899 % 16] = True
+    ref.spoil(step.v, step.vs, free)
+    got = sqp.paged_attention(**step.gpu(), max_q=900, max_len=900).cpu()
+    assert bool(got[899].isnan().all()) and bool(got[:899].isfinite().all())
+    rows = [(0, i, h) for i in (0, 255, 256, 511, 640, 767, 768, 897, 898) for h in (0, 77, 159)]
+    want, tol = step.expected(rows=rows)
+    for b, i, h in rows:
+        assert bool(((got[i, h].double() - want[i, h]).abs() <= tol[i, h]).all()), (i, h)
+
+
+@pytest.mark.parametrize("kind", ["fp16", "e4m3"])
+@pytest.mark.parametrize("B", [9, 64, 65, 150])
+def test_attention_many_sequences(sqp, B, kind):
+    """Ragged batches of more sequences than a wave has lanes, single tokens beside short prompts, some of them unused."""
+    print("case many sequences", B, kind, flush=True)
+    lens = [(37 * b * b + 11 * b) % 190 for b in range(B)]
+    news = [1 if b % 3 or lens[b] < 30 else 17 + b % 13 for b in range(B)]
+    step = ref.Step(lens, news, 6, 2, 64, 16, kind, seed=32)
+    got = sqp.paged_attention(**step.gpu(), max_q=max(news), max_len=max(lens))
+    _compare(step, got)
+    _compare(step, sqp.paged_attention(**step.gpu(), max_q=1, max_len=16))
+
+
 @pytest.mark.parametrize("kind", ["fp16", "e4m3"])
 @pytest.mark.parametrize("lens,news", [([700, 90], [1, 1]), ([700, 300], [40, 130])])
 def test_attention_hints_that_are_too_small(sqp, lens, news, kind):
