@@ -472,3 +472,72 @@ def test_attention_streams_and_graphs(sqp):
             assert torch.equal(held, now)
             step.q = a["q"].cpu()
             _compare(step, given)
+
+
+# ---------------------------------------------------------------- bounds
+
+def _guarded(nbytes, front=256, back=256):
+    """A device buffer with guard bytes on both sides: (whole, the part in between)."""
+    whole = torch.full((front + nbytes + back,), 0xA5, dtype=torch.uint8, device="cuda")
+    return whole, whole[front: front + nbytes]
+
+
+def _intact(whole, nbytes, front=256):
+    return bool((whole[:front] == 0xA5).all()) and bool((whole[front + nbytes:] == 0xA5).all())
+
+
+@pytest.mark.parametrize("kind", ["fp16", "e4m3"])
+@pytest.mark.parametrize("lens,news,heads,kv,D", [([3000, 5, 700], [1, 1, 1], 8, 2, 128), ([2500], [17], 5, 5, 64), ([1500, 900], [33, 900], 8, 2, 128)])
+def test_attention_scratch_of_any_size_and_guards(sqp, lens, news, heads, kv, D, kind):
+    """The output and the scratch stay inside their buffers, and with less scratch than the preferred plan's, or none, the
+    values are still right."""
+    import ctypes
+    L = sqp.lib()
+    step = ref.Step(lens, news, heads, kv, D, 16, kind, seed=40)
+    a, T, B, page, width = step.gpu(), sum(news), len(lens), 16, step.table.shape[1]
+    need = int(L.sqp_paged_attention_scratch_bytes(T, B, heads, kv, D, max(news), max(lens)))
+    P = lambda t: ctypes.c_void_p(t.data_ptr()) if t is not None else None
+    st = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    kind_at = {"fp16": 0, "int8": 1, "e4m3": 2}[kind]
+    for nbytes in sorted({0, need // 3 & ~15, need}):
+        print("case scratch", lens, news, kind, nbytes, need, flush=True)
+        out_w, out = _guarded(T * heads * D * 2)
+        scr_w, scr = _guarded(max(nbytes, 16))
+        rc = L.sqp_paged_attention(T, B, heads, kv, D, kind_at, page, step.k.shape[0], width, max(news), max(lens), D ** -0.5, P(a["q"]), heads * D,
+                                   P(a["k_cache"]), P(a["v_cache"]), P(a["k_scales"]), P(a["v_scales"]), P(a["page_table"]), width, P(a["seq_lens"]),
+                                   P(a["q_starts"]), P(out), P(scr) if nbytes else None, nbytes, st)
+        assert rc == 0
+        torch.cuda.synchronize()
+        assert _intact(out_w, T * heads * D * 2) and _intact(scr_w, max(nbytes, 16))
+        _compare(step, out.view(torch.float16).view(T, heads, D))
+
+
+@pytest.mark.parametrize("kind", ["fp16", "int8", "e4m3"])
+def test_cache_and_norm_guards(sqp, kind):
+    """Writes stay inside the outputs on odd sizes."""
+    T, heads, kv, D, page, pages = 7, 3, 1, 64, 16, 2
+    qkv, slots, positions, *_ = _cache_inputs(T, heads, kv, D, page, kind)
+    q, k, v = _parts(qkv.cuda(), heads, kv, D)
+    dt = ref.TYPES[kind]
+    size = pages * kv * page * D * (2 if kind == "fp16" else 1)
+    bufs = [_guarded(size), _guarded(size), _guarded(pages * kv * page * 4), _guarded(pages * kv * page * 4), _guarded(T * heads * D * 2)]
+    kc, vc = [b[1].view(dt).view(pages, kv, page, D) for b in bufs[:2]]
+    ks, vs = [b[1].view(torch.float32).view(pages, kv, page) if kind != "fp16" else None for b in bufs[2:4]]
+    slots = torch.tensor([0, 31, 15, 16, 40, -3, 7], dtype=torch.int32).cuda()
+    sqp.kv_cache_write(k, v, slots, kc, vc, ks, vs, q=q, cos_sin=ref.cos_sin_table(5000, D).cuda(), positions=positions.cuda(),
+                       out=bufs[4][1].view(torch.float16).view(T, heads, D))
+    rk, rv = _guarded(T * kv * D * 2), _guarded(T * kv * D * 2)
+    sqp.kv_cache_read(slots, kc, vc, ks, vs, out=[b[1].view(torch.float16).view(T, kv, D) for b in (rk, rv)])
+    torch.cuda.synchronize()
+    for whole, part in bufs + [rk, rv]:
+        assert _intact(whole, part.numel())
+    M, H = 3, 2056
+    x, res, gamma = _norm_inputs(M, H, 50)
+    y, r, c, s = _guarded(M * H * 2), _guarded(M * H * 2), _guarded(M * H), _guarded(16)
+    half = lambda b: b[1].view(torch.float16).view(M, H)
+    sqp.add_rmsnorm(x.cuda(), res.cuda(), gamma.cuda(), 1e-5, out=half(y), sum_out=half(r))
+    if kind != "fp16":
+        sqp.add_rmsnorm_quant(x.cuda(), res.cuda(), gamma.cuda(), 1e-5, dt, out=(c[1].view(dt).view(M, H), s[1].view(torch.float32)[:M]), sum_out=half(r))
+    torch.cuda.synchronize()
+    for whole, part in (y, r, c, s):
+        assert _intact(whole, part.numel())
