@@ -311,6 +311,22 @@ __device__ __forceinline__ int sqp_wave_sum(int x)
     return __builtin_amdgcn_readlane(x, 15) + __builtin_amdgcn_readlane(x, 31) + __builtin_amdgcn_readlane(x, 47) + __builtin_amdgcn_readlane(x, 63);
 }
 
+// The same for floats, and the largest (a lane exchange through the data-sharing unit takes a hundred cycles a step, these a few).
+template <bool MAX>
+__device__ __forceinline__ float sqp_wave_join(float x)
+{
+    auto lane = [](float v, int i) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i)); };
+    auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+    const int none = __builtin_bit_cast(int, MAX ? SQP_LOWEST : 0.f);
+#define SQP_ROW_SHR(n) x = join(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(none, __builtin_bit_cast(int, x), 0x110 + n, 0xf, 0xf, false)))
+    SQP_ROW_SHR(1);
+    SQP_ROW_SHR(2);
+    SQP_ROW_SHR(4);
+    SQP_ROW_SHR(8);
+#undef SQP_ROW_SHR
+    return join(join(lane(x, 15), lane(x, 31)), join(lane(x, 47), lane(x, 63)));
+}
+
 // The tile (of `height` rows) that is rank-th in the order of work, over all sequences of more than above_rows rows: those first
 // that see most, so that the long ones do not begin last.  From `fold` on the order is turned round: with as many
 // workgroups as fit the chip at once, the shortest share their compute units with the longest.  b < 0: no such tile.
@@ -340,10 +356,14 @@ __device__ __forceinline__ SqpTile sqp_pick_tile(const SqpAttention &a, int abov
         }
         return {-1, 0};
     }
-    const int n = lane < a.B ? tiles_of(lane) : 0, all = a.B == 1 ? __builtin_amdgcn_readlane(n, 0) : sqp_wave_sum(n);
+    if (a.B == 1) {
+        const int rows = sqp_one_sequence(a, 0).n * a.group, all = rows > above_rows ? (rows + height - 1) / height : 0;
+        if (rank >= all) return {-1, 0};
+        return {0, fold > 0 && rank >= fold ? rank - fold : all - 1 - rank};
+    }
+    const int n = lane < a.B ? tiles_of(lane) : 0, all = sqp_wave_sum(n);
     if (rank >= all) return {-1, 0};
     if (fold > 0 && rank >= fold) rank = all - 1 - (rank - fold);
-    if (a.B == 1) return {0, all - 1 - rank};
     // A tile's key: its sequence's length, less a power of two near the tokens per tile for every tile behind it.
     int shift = 0;
     while ((a.group << (shift + 1)) <= height) shift++;

@@ -31,6 +31,9 @@ __device__ __forceinline__ uint4 add8(const uint4 a, const uint4 b)
 // One workgroup of W waves per row, NI pieces of 8 values per thread, which stay in registers between the sum of squares and
 // the scaling: x, the residual and gamma are read once.  The largest |r gamma| is found in the same pass as the sum of squares
 // (it is the largest |y| up to the row's factor), so that the 8-bit output needs no second exchange between the waves.
+// Bound: few rows, the launch and a chain of latencies (2.2 us on 1 x 4096); many, HBM (2048 x 8192 read twice and written twice in
+// 20.8 us, 6.4 TB/s; with e4m3 output 20.5 us).  A row is spread over up to 16 waves at any number of rows: with 4 waves
+// 512 x 8192 takes 8.3 us instead of 7.4, 4096 x 8192 45.5 instead of 43.0 (e4m3: 39.3 instead of 41).
 template <int W, int NI, int OUT>
 __global__ void __launch_bounds__(64 * W) add_rmsnorm_kernel(int H8, float inv_h, float eps, const uint4 *x, const uint4 *residual,
                                                              const uint4 *__restrict__ gamma, void *__restrict__ y, float *__restrict__ scales, uint4 *sum)

@@ -246,7 +246,7 @@ ATTENTION_CASES = [  # cached tokens, new tokens, heads, kv_heads, D, page
     ([64], [64], 4, 4, 128, 64),
     ([200], [200], 6, 2, 64, 16),
     ([333, 50, 128], [129, 50, 1], 8, 1, 128, 16),
-    ([517, 65, 64, 0, 90], [33, 1, 64, 1, 32], 24, 4, 128, 32),
+    ([517, 65, 64, 0, 90], [33, 1, 64, 1, 32], 20, 4, 128, 32),
     ([1300], [70], 16, 2, 64, 128),
     ([400, 3], [1, 3], 2, 2, 128, 16),
     ([2600], [17], 5, 5, 128, 64),
