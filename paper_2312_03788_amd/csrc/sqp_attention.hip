@@ -136,7 +136,7 @@ extern "C" int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D,
     if (!q || !page_table || !seq_lens || !out) return SQP_ERR_NULL;
     if (T < 0 || B < 0 || B > 65535 || heads <= 0 || heads > 65535 || (heads % kv_heads) || max_q < 0 || max_len < 0) return SQP_ERR_SHAPE;
     if ((!q_starts && T != B) || (B == 0 && T > 0)) return SQP_ERR_SHAPE;
-    if (table_width <= 0 || (long)table_width * page >= (1L << 31) || (B > 1 && table_stride < table_width)) return SQP_ERR_SHAPE;
+    if (table_width <= 0 || (long)table_width * page > (1L << 30) || (B > 1 && table_stride < table_width)) return SQP_ERR_SHAPE;
     if (q_stride < (long)heads * D || sqp_too_big(T, (long)heads * D)) return SQP_ERR_SHAPE;
     if (!(scale > 0.0f) || !(scale < 1e30f)) return SQP_ERR_ARG;
     if ((q_stride % 8) || sqp_misaligned(q) || sqp_misaligned(out) || (scratch && sqp_misaligned(scratch))) return SQP_ERR_ALIGN;

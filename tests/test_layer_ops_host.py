@@ -86,7 +86,7 @@ def test_cache_refusals(L):
 def test_attention_refusals(L):
     for bad in (dict(q=null), dict(table=null), dict(lens=null), dict(out=null)):
         assert _attend(L, **bad) == NULL
-    for bad in (dict(heads=7), dict(heads=0), dict(B=-1), dict(B=1 << 16), dict(B=0), dict(max_q=-1), dict(max_len=-1), dict(starts=null), dict(width=0), dict(width=1 << 27),
+    for bad in (dict(heads=7), dict(heads=0), dict(B=-1), dict(B=1 << 16), dict(B=0), dict(max_q=-1), dict(max_len=-1), dict(starts=null), dict(width=0), dict(width=1 << 27), dict(width=(1 << 26) + 1, ts=1 << 27),
                 dict(ts=2), dict(qs=1016), dict(T=1 << 22)):
         assert _attend(L, **bad) == SHAPE, bad
     for bad in (dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))):
