@@ -276,7 +276,8 @@ int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages,
  * q_starts[b] .. q_starts[b + 1] - 1 of q (q_starts [B + 1], not decreasing; NULL: T == B, one token each).  The i-th of its n
  * new tokens sees the tokens j <= seq_lens[b] - n + i.  A token that sees nothing, or belongs to no sequence, gets zeros.
  *   q [T][heads][D] fp16, q_stride elements between tokens; out [T][heads][D] fp16
- *   page_table [B][table_width] int32 (table_width * page <= 2^30), table_stride entries between rows; entries past a sequence's length may be anything
+ *   page_table [B][table_width] int32, table_width * page <= 2^30, table_stride entries between rows; entries past a
+ *                   sequence's length may be anything
  *   max_q, max_len  the most new tokens and the greatest length of a sequence, as far as the caller knows: the work is laid
  *                   out by them.  Larger ones in the arrays are computed as well, only slower.  0: not known
  *                   (scratch_bytes: max_len = table_width * page then; max_q = 1 without q_starts).
