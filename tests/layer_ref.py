@@ -112,7 +112,7 @@ class Step:
         x = cache.view(torch.uint8)[pages, :, place].view(cache.dtype) if cache.dtype == torch.float8_e4m3fn else cache[pages, :, place]
         return dequantised(x, None if scales is None else scales[pages, :, place]).transpose(0, 1)
 
-    def expected(self, scale=None, rows=None):
+    def expected(self, scale=None, rows=None, p_error=2.0 ** -11, rounded=True):
         """(out, tolerance) [T, heads, D] in 64 bits (rows: (sequence, new token, head) to compute, the others are left zero).
 
         The kernels hold scores, sums and outputs in fp32 and round p to fp16 once, the output once.  With A = sum_j p_j |v_j|:
@@ -120,10 +120,11 @@ class Step:
           p's rounding            2^-11 A, and half of the smallest step per token where p is far below the row's largest
           scores                  a score of D products is off by at most (D + 8) 2^-24 sum_d |q_d k_d| scale, the power of two
                                   by 2^-21: a p by that share, the numerator and the denominator both
-          sums over the tokens    len 2^-24 each"""
+          sums over the tokens    len 2^-24 each
+        (p_error: p's share; rounded=False: without the output's rounding.)"""
         scale = self.D ** -0.5 if scale is None else scale
         T = self.q.shape[0]
-        out, tol = torch.zeros((T, self.heads, self.D), dtype=torch.float64), torch.full((T, self.heads, self.D), 2.0 ** -25, dtype=torch.float64)
+        out, tol = torch.zeros((T, self.heads, self.D), dtype=torch.float64), torch.full((T, self.heads, self.D), 2.0 ** -25 if rounded else 0.0, dtype=torch.float64)
         group = self.heads // self.kv_heads
         for b, (length, n) in enumerate(zip(self.lens, self.news)):
             if length == 0:
@@ -145,5 +146,5 @@ class Step:
                     o, A = p @ vh[:m], p @ vh[:m].abs()
                     e = (self.D + 8) * 2.0 ** -24 * float(size.max()) + 2.0 ** -21
                     out[first + i, h] = o
-                    tol[first + i, h] += 2.0 ** -11 * o.abs() + (2.0 ** -11 + 2 * e + m * 2.0 ** -23) * A + m * 2.0 ** -25 * p.max() * vh[:m].abs().max()
+                    tol[first + i, h] += (2.0 ** -11 * o.abs() if rounded else 0.0) + (p_error + 2 * e + m * 2.0 ** -23) * A + m * 2.0 ** -25 * p.max() * vh[:m].abs().max()
         return out, tol
