@@ -109,16 +109,6 @@ __device__ __forceinline__ uint32_t sqp_pair(const uint32_t *a, const uint32_t *
     }
 }
 
-// Whether a word holds a value that is not finite.
-template <int TYPE>
-__device__ __forceinline__ bool sqp_not_finite(uint32_t w)
-{
-    if constexpr (TYPE == SQP_FP16) return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
-    if constexpr (TYPE == SQP_E4M3)
-        return (w & 0x7fu) == 0x7fu || (w & 0x7f00u) == 0x7f00u || (w & 0x7f0000u) == 0x7f0000u || (w & 0x7f000000u) == 0x7f000000u;
-    return false;
-}
-
 // An index array's element at the same place for a whole wave, through the scalar cache (no kernel writes these arrays).
 __device__ __forceinline__ int sqp_uniform(const int *p) { return *(const __attribute__((address_space(4))) int *)(uintptr_t)p; }
 
@@ -264,8 +254,8 @@ __device__ __forceinline__ void sqp_attend_row(const SqpAttention &a, const h16 
     }
 }
 
-// The same for a row of a part, result included: the slow way of the kernels below where a value that only some of their rows
-// see is infinite or NaN (zero times it is not zero, so the matrix instructions cannot mask it).
+// The same for a row of a part, result included: the slow way of the kernels below where a value is infinite or NaN (zero times
+// it is not zero, so the matrix instructions cannot keep it from the rows that do not see it).
 template <int TYPE, int D>
 __device__ __forceinline__ void sqp_attend_row_of_part(const SqpAttention &a, const SqpParts &parts, int part, int token, int head, int sees, const int *table_row, int lo,
                                                        int hi)

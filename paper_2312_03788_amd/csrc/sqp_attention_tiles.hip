@@ -22,7 +22,7 @@
 // Measured: 2048 tokens behind 14336, 64 heads on 8, e4m3: 1070 to 1160 us from box to box, 890 to 960 TFLOP/s, where a large dense
 // fp16 product of the library reaches 1134 and a loop of matrix instructions alone 1572: all of them run at the clock that the
 // power limit leaves (1.8 of 2.4 GHz here).  A tile of 64 tokens takes a compute unit 2.2 to 2.35 us; without staging, maxima,
-// exponentials and barriers it still takes 1.8 to 2.0.  A 2048-token prompt of 32 heads: 61 us; its longest tile goes through
+// exponentials and barriers it still takes 1.8 to 2.0.  A 2048-token prompt of 32 heads: 57.5 us; its longest tile goes through
 // 32 steps of 64 tokens alone on its compute unit at 1.4 to 1.9 us each, in which latencies show that a second wave would hide.
 // Dropped: 64 rows per wave with one wave per SIMD (half the reads of shared memory, but nothing hides what the order of
 // instructions does not: 1288 us where 128-row tiles took 1240); stores spread over a step (their loads have less time: the
@@ -52,7 +52,6 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
     __shared__ __attribute__((aligned(16))) h16 s_k[2][64 * KROW];
     __shared__ __attribute__((aligned(16))) h16 s_v[VBUFS][D * VROW];
     __shared__ __attribute__((aligned(16))) float s_ks[2][64], s_lv[2][64], s_rv[VBUFS][64];
-    __shared__ int s_bad;
 
     const int kv_head = blockIdx.x, part = blockIdx.y % parts.parts, ranks = gridDim.y / parts.parts;
     if (blockIdx.y == 0) sqp_zero_strays<D>(a, kv_head);
@@ -71,7 +70,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         const int *table = a.table + b * a.table_stride;
         const int before = s.len - s.n;  // token i of the new ones sees before + i + 1
         const int row0 = tile * ROWS, row_last = min(row0 + ROWS, rows) - 1;
-        const int most = before + row_last / a.group + 1, least = before + row0 / a.group + 1;
+        const int most = before + row_last / a.group + 1;
         const int nparts = parts.of(most);
         if (part >= nparts) continue;
         const int lo = part * parts.chunk, hi = part == nparts - 1 ? most : lo + parts.chunk;
@@ -90,7 +89,6 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         // ---- staging; pages are looked up a tile ahead
         uint32_t kw[4 * KL], vw[8 * VW];
         float kscale = 0.f, kvscale = 0.f, vscale = 0.f;
-        bool bad = false;
         auto place = [&](int base) { return min(base + 16 * block16, (hi - 1) & ~15); };
         auto look_up = [&](int base) { return lo < hi ? sqp_page(a, table, place(base)) : 0; };
         auto cache_row = [&](int page, int base) {
@@ -130,27 +128,20 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
                 if (piece == KPIECES - 1 && lane < TOKENS) {
                     s_ks[buf][16 * block16 + first_token + lane] = kscale * a.scale2;
                     const float x = fmaxf(kvscale, 0x1p-100f);
-                    s_lv[buf][16 * block16 + first_token + lane] = kvscale == kvscale ? __builtin_amdgcn_logf(x) : kvscale;
+                    s_lv[buf][16 * block16 + first_token + lane] = kvscale >= 0.f ? __builtin_amdgcn_logf(x) : __builtin_nanf("");
                 }
             } else {
                 *(u32x4 *)&to[8 * (unit % KU)] = u32x4{kw[4 * i], kw[4 * i + 1], kw[4 * i + 2], kw[4 * i + 3]};
             }
         };
-        // Tokens past the length (whatever memory holds there), and values that not all rows see and that are not finite.
-        auto inspect_v = [&](int base) {
-            if (__builtin_expect(base + 64 > least, 0)) {
+        // Tokens past the length, whatever memory holds there.
+        auto clear_v = [&](int base) {
+            if (__builtin_expect(base + 64 > s.len, 0)) {
 #pragma unroll
                 for (int j = 0; j < 8; j++) {
                     const int key = base + 16 * block16 + 8 * (j >> 2) + 4 * v_half + (j & 3);
 #pragma unroll
-                    for (int e = 0; e < VW; e++) {
-                        if (key >= s.len) vw[j * VW + e] = 0;
-                        else bad = bad || sqp_not_finite<TYPE>(vw[j * VW + e]);
-                    }
-                }
-                if constexpr (CODES) {
-                    if (base + 16 * block16 + first_token + lane % TOKENS >= s.len) vscale = 0.f;
-                    bad = bad || !(__builtin_fabsf(vscale) < INFINITY);
+                    for (int e = 0; e < VW; e++) vw[j * VW + e] = key >= s.len ? 0 : vw[j * VW + e];
                 }
             }
         };
@@ -301,7 +292,6 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
             }
         };
 
-        if (threadIdx.x == 0) s_bad = 0;
         if (lo < hi) {  // the first tile, and the second one's K; the third one's K and the second one's V are on their way then
             load_k(lo);
             load_v(lo);
@@ -311,7 +301,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
 #pragma unroll
             for (int i = 0; i < 4 * KL; i++) first_kw[i] = kw[i];
             load_k(lo + 64);
-            inspect_v(lo);
+            clear_v(lo);
 #pragma unroll
             for (int i = 0; i < VD; i++) store_v(0, i);
             load_v(lo + 64);
@@ -349,7 +339,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         for (int base = lo; base < hi; base += 64) {
             const int vnext = vbuf == VBUFS - 1 ? 0 : vbuf + 1;
             const bool active = base < wave_most;
-            inspect_v(base + 64);
+            clear_v(base + 64);
             auto keep_v = [&](int i) { store_v(vnext, i); };
             if (active) {
                 step(t, u, vbuf, 0, kbuf, 1, VD, keep_v);
@@ -375,10 +365,18 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         }
         l += l2;
         l += __shfl_xor(l, 32, 64);
-        if (bad) s_bad = 1;
-        __syncthreads();
-        if (s_bad) {
-            for (int r = row0 + wave; r <= row_last; r += W) {
+        // A value that is infinite or NaN makes NaN of the rows that do not see it too (zero times it), and so does one whose p
+        // is too small for fp16, and any whose scale is negative: then the wave's rows are computed one by one.
+        float all = 0.f;
+#pragma unroll
+        for (int d = 0; d < NV; d++) {
+            float some = o[d][0];
+#pragma unroll
+            for (int r = 1; r < 16; r++) some += o[d][r];  // (finite ones stay far below the largest float)
+            all += some;
+        }
+        if (__any(!(__builtin_fabsf(all) < INFINITY))) {
+            for (int r = wave_row; r <= min(wave_row + 31, row_last); r++) {
                 const int tk = r / a.group;
                 sqp_attend_row_of_part<TYPE, D>(a, parts, part, s.first + tk, kv_head * a.group + r - tk * a.group, before + tk + 1, table, lo, hi);
             }
@@ -413,7 +411,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
                 }
             }
         }
-        __syncthreads();  // (s_bad and the tiles are written again for the next rows)
+        __syncthreads();  // (the tiles are written again for the next rows)
     }
 }
 

@@ -274,6 +274,58 @@ def test_attention(sqp, case, kind):
 
 @pytest.mark.parametrize("kind", ["fp16", "int8", "e4m3"])
 @pytest.mark.parametrize("heads,kv,D,lens,news", [
+    (8, 2, 128, [1, 7, 40, 300], [1] * 4), (16, 1, 64, [2, 90, 33], [1] * 3), (4, 2, 128, [90, 8], [3, 8]), (8, 8, 64, [1500], [1])])
+def test_attention_of_few_rows_rounds_once(sqp, heads, kv, D, lens, news, kind):
+    """Up to 16 rows per cached head take p in two parts of 11 bits (2^-22 of it), so that the output's rounding is the only one to fp16.
+    With x what is rounded and w the formula's value, fp16(x) is nearest to x: |fp16(x) - w| <= |fp16(w) - w| + 2 |x - w|.  Scores
+    are small here, so that their own errors are."""
+    print("case rounds once", heads, kv, D, lens, news, kind, flush=True)
+    step = ref.Step(lens, news, heads, kv, D, 16, kind, seed=33, q_scale=0.01)
+    got = sqp.paged_attention(**step.gpu(), max_q=max(news), max_len=max(lens)).cpu().double()
+    want, tol = step.expected(p_error=2.0 ** -22, rounded=False)
+    assert bool(((got - want).abs() <= (want.half().double() - want).abs() + 2 * tol).all())
+
+
+@pytest.mark.parametrize("kind", ["fp16", "int8", "e4m3"])
+@pytest.mark.parametrize("lens,news", [([40], [1]), ([40, 600, 9], [1, 1, 1]), ([40, 60], [2, 1]), ([60, 700], [40, 50]), ([300], [150])])
+def test_attention_of_infinite_values(sqp, lens, news, kind):
+    """A value (in 8 bits: its scale) that is infinite gives the outputs that the formula gives: infinities of its signs, NaN where a
+    code of zero is scaled by it, and what is beside it is untouched."""
+    print("case infinite values", lens, news, kind, flush=True)
+    step = ref.Step(lens, news, 8, 2, 128, 16, kind, seed=34, q_scale=0.1)
+    page, place = int(step.table[0, 1]), 3          # token 19 of the first sequence, which all of its new tokens see
+    if kind == "fp16":
+        step.v[page, 1, place, ::5] = float("inf")
+        step.v[page, 1, place, 1::5] = float("-inf")
+    else:
+        step.vs[page, 1, place] = float("inf")
+    got = sqp.paged_attention(**step.gpu(), max_q=max(news), max_len=max(lens)).cpu().double()
+    want, tol = step.expected()
+    fine = want.isfinite()
+    assert bool((~fine).any()) and bool(fine.any())
+    assert bool(((got[fine] - want[fine]).abs() <= tol[fine]).all())
+    assert torch.equal(got[~fine].nan_to_num(nan=0.0, posinf=1.0, neginf=-1.0), want[~fine].nan_to_num(nan=0.0, posinf=1.0, neginf=-1.0))
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("lens,news", [([40, 600], [1, 1]), ([300, 70], [150, 9])])
+def test_attention_of_scales_of_either_sign_and_not_a_number(sqp, lens, news, kind):
+    """A scale is a factor like any other: negative ones (which the write does not make), zero, and NaN where a token is seen."""
+    print("case scales", lens, news, kind, flush=True)
+    step = ref.Step(lens, news, 8, 2, 128, 16, kind, seed=35)
+    for scales in (step.ks, step.vs):
+        scales[..., 1::3] *= -1.0
+        scales[..., 5::7] = 0.0
+    step.vs[int(step.table[0, 1]), 1, 4] = float("nan")  # token 20 of the first sequence, second cached head
+    got = sqp.paged_attention(**step.gpu(), max_q=max(news), max_len=max(lens)).cpu().double()
+    want, tol = step.expected()
+    lost = want.isnan()
+    assert torch.equal(got.isnan(), lost) and bool(lost[: news[0], 4:].all()) and int(lost.sum()) == news[0] * 4 * 128
+    assert bool(((got - want).abs() <= tol)[~lost].all())
+
+
+@pytest.mark.parametrize("kind", ["fp16", "int8", "e4m3"])
+@pytest.mark.parametrize("heads,kv,D,lens,news", [
     (32, 32, 64, [4096], [4096]),                       # as many tiles as take the 256-row form, one sequence
     (64, 8, 128, [2300, 1500], [1100, 1029]),           # and two
     (64, 16, 128, [600, 2111, 33, 700], [600, 1, 33, 500]),
