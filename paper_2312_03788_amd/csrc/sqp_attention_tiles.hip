@@ -26,7 +26,9 @@
 // 32 steps of 64 tokens alone on its compute unit at 1.4 to 1.9 us each, in which latencies show that a second wave would hide.
 // Dropped: 64 rows per wave with one wave per SIMD (half the reads of shared memory, but nothing hides what the order of
 // instructions does not: 1288 us where 128-row tiles took 1240); stores spread over a step (their loads have less time: the
-// prompt 68.6 -> 74.6 us); K in shared memory with its scale multiplied in (a rounding more in the scores).
+// prompt 68.6 -> 74.6 us); K in shared memory with its scale multiplied in (a rounding more in the scores); p cut to 11 bits before
+// the sum takes it too, so that its error leaves rows that a few tokens rule (worst of 70 cases 1.37 times the output's rounding
+// instead of 1.45, but the chunk 1090 -> 1119 us).
 #include <algorithm>
 
 #include "sqp_attention.h"
