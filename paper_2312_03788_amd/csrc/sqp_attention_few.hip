@@ -9,16 +9,17 @@
 //                 without leaving its lane: token 4g + j (j < 4) of either 16 is slot (g, j), g the lane's row of 16.  V^T's operand
 //                 wants 8 tokens' values of one dimension in a lane: a lane loads D / 16 dimensions of its 8 tokens (a load of
 //                 16 lanes is a token's whole row) and pairs tokens up with one byte permutation per word.
-// So nothing goes through shared memory but the four waves' results.  The matrix cores wait for memory here, so p goes through them twice: rounded to fp16, and what that leaves, in fp16 again (2^-22 of
-// p then).  The output's rounding is the only one left: the error of 8192-token outputs is 2.1e-4 of them instead of 3.0e-4, in the
-// same time (45.0 and 45.1 us with the 16 sequences below, 147.0 and 147.1 with the 32).
-// Registers hold a step's K and V while the next one's are on
+// So nothing goes through shared memory but the four waves' results.  Registers hold a step's K and V while the next one's are on
 // their way: 64 KB per compute unit, two workgroups of four waves.  With three (168 registers) values spill and 32 sequences
 // at up to 2500 tokens take 286 us instead of 147.
 //
+// The matrix cores wait for memory here, so p goes through them twice: rounded to fp16, and what that leaves, in fp16 again (2^-22
+// of p then).  The output's rounding is the only one left: the error of 8192-token outputs is 2.1e-4 of them instead of 3.0e-4, in
+// the same time (45.0 and 45.1 us with the 16 sequences below, 147.0 and 147.1 with the 32).
+//
 // Measured, kernel alone: those 800 MB in 146 us (5.5 TB/s; a streaming read alone reaches 5.9 on this chip); one sequence of 32000
-// tokens, 40 heads, int8, 338 MB in 59 us (5.7 TB/s); 16 at up to 8192, 8 cached heads, e4m3, 166 MB in 34 us (4.9 TB/s, parts of
-// unequal length).  32 heads over 129 tokens: 6.6 us, the chain length, page, K, V.
+// tokens, 40 heads, int8, 338 MB in 59 us (5.7 TB/s); 16 at up to 8192, 8 cached heads, e4m3, 166 MB in 34 to 37 us from box to box (4.9 TB/s,
+// parts of unequal length).  32 heads over 129 tokens: 6.2 us, the chain length, page, K, V.
 #include "sqp_attention.h"
 
 namespace {
