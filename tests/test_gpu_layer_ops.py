@@ -293,6 +293,7 @@ def test_attention_of_infinite_values(sqp, lens, news, kind):
     code of zero is scaled by it, and what is beside it is untouched."""
     print("case infinite values", lens, news, kind, flush=True)
     step = ref.Step(lens, news, 8, 2, 128, 16, kind, seed=34, q_scale=0.1)
+    tol = step.expected()[1]                        # (as without the infinities, which are in dimensions of their own)
     page, place = int(step.table[0, 1]), 3          # token 19 of the first sequence, which all of its new tokens see
     if kind == "fp16":
         step.v[page, 1, place, ::5] = float("inf")
@@ -300,11 +301,28 @@ def test_attention_of_infinite_values(sqp, lens, news, kind):
     else:
         step.vs[page, 1, place] = float("inf")
     got = sqp.paged_attention(**step.gpu(), max_q=max(news), max_len=max(lens)).cpu().double()
-    want, tol = step.expected()
+    want, _ = step.expected()
     fine = want.isfinite()
     assert bool((~fine).any()) and bool(fine.any())
     assert bool(((got[fine] - want[fine]).abs() <= tol[fine]).all())
     assert torch.equal(got[~fine].nan_to_num(nan=0.0, posinf=1.0, neginf=-1.0), want[~fine].nan_to_num(nan=0.0, posinf=1.0, neginf=-1.0))
+
+
+@pytest.mark.parametrize("lens,news", [([40, 9], [1, 1]), ([40], [3]), ([300, 70], [150, 9])])
+def test_attention_of_codes_that_are_not_numbers(sqp, lens, news):
+    """A NaN among e4m3's codes makes NaN of its dimension (a value) or its token's score (a key), of the rows that see it."""
+    print("case codes not numbers", lens, news, flush=True)
+    for what, at in (("v", 20), ("v", lens[0] - 1), ("k", lens[0] - 1)):
+        step = ref.Step(lens, news, 8, 2, 128, 16, "e4m3", seed=36)
+        tol = step.expected()[1]  # (as without the NaN, which is in one dimension, or in all of a lost row)
+        getattr(step, what).view(torch.uint8)[int(step.table[0, at // 16]), 1, at % 16, 77] = 0x7f
+        got = sqp.paged_attention(**step.gpu(), max_q=max(news), max_len=max(lens)).cpu().double()
+        want, _ = step.expected()
+        lost = want.isnan()
+        rows = news[0] if at == 20 else 1
+        assert int(lost.sum()) == rows * 4 * (1 if what == "v" else 128)
+        assert torch.equal(got.isnan(), lost)
+        assert bool(((got - want).abs() <= tol)[~lost].all())
 
 
 @pytest.mark.parametrize("kind", ["int8", "e4m3"])
