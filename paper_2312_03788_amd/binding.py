@@ -599,7 +599,8 @@ def paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts=None, k_
     values already: fp16 [T, heads, D].  page_table int32 [B, pages of a sequence], seq_lens int32 [B] (cached tokens, the new
     ones among them), q_starts int32 [B + 1] (None: one new token per sequence).  max_q, max_len: the most new tokens and the
     greatest length, if the caller knows them (the work is laid out by them; larger ones are right, only slower).  scale: of the
-    scores, D^-0.5 by default."""
+    scores, D^-0.5 by default.  Under graph capture a call with `out` allocates nothing, so that long sequences are not split over
+    workgroups (few of them take several times as long); without it the output and the scratch come from the graph's pool."""
     if _fast is not None and isinstance(q, _Tensor) and q.is_cuda:
         dev = _current_device()
         o = _fast.paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts, k_scales, v_scales, max_q, max_len, scale, out, dev, _raw_stream(dev))
