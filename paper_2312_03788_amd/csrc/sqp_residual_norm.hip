@@ -28,6 +28,18 @@ __device__ __forceinline__ uint4 add8(const uint4 a, const uint4 b)
     return __builtin_bit_cast(uint4, s);
 }
 
+// The scale of a row whose largest |r gamma| has these bits, r the row's factor, and what takes r gamma to codes: y / scale
+// = r gamma MAX / max |r gamma| is free of the row's factor, and r gamma is exact in fp32 (11 bits by 11), so that a code is
+// two roundings away from the formula's value and not five (of 16.8 million e4m3 codes 43 fall on the other side of a rounding's
+// edge, four inputs' mean, and 57 with five).
+template <int OUT>
+__device__ __forceinline__ void row_codes(uint32_t amax, float r, float &step, float &inverse)
+{
+    const float most = __builtin_bit_cast(float, amax), a = most * r;  // NaN where the row holds no finite sum
+    sqp_row_step<OUT>(sqp_abs_bits(a), step, inverse);
+    if (inverse != 0.f) inverse = SqpCode<OUT>::MAX / most;
+}
+
 // One workgroup of W waves per row, NI pieces of 8 values per thread, which stay in registers between the sum of squares and
 // the scaling: x, the residual and gamma are read once.  The largest |r gamma| is found in the same pass as the sum of squares
 // (it is the largest |y| up to the row's factor), so that the 8-bit output needs no second exchange between the waves.
@@ -84,8 +96,7 @@ __global__ void __launch_bounds__(64 * W) add_rmsnorm_kernel(int H8, float inv_h
     if constexpr (OUT != HALF) {
 #pragma unroll
         for (int i = 0; i < W; i++) amax = max(amax, top[i]);
-        const float a = __builtin_bit_cast(float, amax) * r;  // NaN where the row holds no finite sum
-        sqp_row_step<OUT>(sqp_abs_bits(a), step, inverse);
+        row_codes<OUT>(amax, r, step, inverse);
         if (threadIdx.x == 0) scales[blockIdx.x] = step;
     }
 #pragma unroll
@@ -96,7 +107,7 @@ __global__ void __launch_bounds__(64 * W) add_rmsnorm_kernel(int H8, float inv_h
             sqp_widen8(v[j], f);
             sqp_widen8(g[j], gf);
 #pragma unroll
-            for (int e = 0; e < 8; e++) f[e] = f[e] * r * gf[e];
+            for (int e = 0; e < 8; e++) f[e] = OUT == HALF ? f[e] * r * gf[e] : f[e] * gf[e];
             if constexpr (OUT == HALF) ((uint4 *)y)[row + i] = sqp_narrow8(f);
             else ((uint2 *)y)[row + i] = sqp_codes8<OUT>(f, inverse);
         }
@@ -137,8 +148,7 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_long_kernel(int H8, float in
     float step = 0.f, inverse = 0.f;
     if constexpr (OUT != HALF) {
         for (int i = 0; i < 16; i++) amax = max(amax, top[i]);
-        const float a = __builtin_bit_cast(float, amax) * r;
-        sqp_row_step<OUT>(sqp_abs_bits(a), step, inverse);
+        row_codes<OUT>(amax, r, step, inverse);
         if (threadIdx.x == 0) scales[blockIdx.x] = step;
     }
     for (int i = threadIdx.x; i < H8; i += 1024) {
@@ -146,7 +156,7 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_long_kernel(int H8, float in
         sqp_widen8(sum[row + i], f);
         sqp_widen8(gamma[i], gf);
 #pragma unroll
-        for (int e = 0; e < 8; e++) f[e] = f[e] * r * gf[e];
+        for (int e = 0; e < 8; e++) f[e] = OUT == HALF ? f[e] * r * gf[e] : f[e] * gf[e];
         if constexpr (OUT == HALF) ((uint4 *)y)[row + i] = sqp_narrow8(f);
         else ((uint2 *)y)[row + i] = sqp_codes8<OUT>(f, inverse);
     }
