@@ -251,6 +251,7 @@ __device__ __forceinline__ void sqp_attend_row(const SqpAttention &a, const h16 
                 if constexpr (PER == 2) o[1] += pj * (float)x.y;
             }
         }
+        if (__all(o[0] != o[0] && o[PER - 1] != o[PER - 1])) break;  // NaN as a whole, whatever follows
     }
 }
 
