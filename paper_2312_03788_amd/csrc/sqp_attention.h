@@ -46,6 +46,16 @@ constexpr float SQP_LOWEST = -3e38f;  // the running maximum of a row that has s
 
 __device__ __forceinline__ float sqp_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A value's scale in the exponent of its token's weight: its logarithm, of 2^-40 at least (any code times that is below half of
+// fp16's smallest number), so that a token of tiny or zero values keeps its place in the sum of the weights.
+__device__ __forceinline__ float sqp_log_scale(float scale) { return __builtin_amdgcn_logf(fmaxf(scale, 0x1p-40f)); }
+
+// NaN for a scale that the exponent does not take, negative or from 2^40 on (or NaN): it shows in the sums, and leads to the slow way.
+__device__ __forceinline__ float sqp_known_scale(float scale)
+{
+    return __builtin_bit_cast(uint32_t, scale) < 0x53800000u ? scale : __builtin_nanf("");
+}
+
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // BYTES bytes as words.

@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             }
         };
 
-        float m = SQP_LOWEST, l = 0.f, lv = TYPE == SQP_FP16 ? 0.f : -60.f;
+        float m = SQP_LOWEST, l = 0.f;
         f32x4 o[DPL];
 #pragma unroll
         for (int t = 0; t < DPL; t++) o[t] = (f32x4)(0.f);
@@ -134,7 +134,6 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             const bool more = base + 64 * NB < hi;
             look_up(base + 128 * NB, ahead);
             if (more) load_k(base + 64 * NB, page);
-            float vmax = 0.f;
             if (base + 16 * NB > fewest) {  // some row does not see all of these tokens
 #pragma unroll
                 for (int i = 0; i < 4 * NB; i++) {
@@ -147,24 +146,23 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                     }
                 }
             }
-            float top = t[0];
+            // What goes through the matrix cores is p times the value's scale, so the running maximum is taken of that: t + log2 of
+            // the token's own scale.  It stays below 2^15, inside fp16's range, with the maximum changed only now and then.
+            float top = -INFINITY;
 #pragma unroll
-            for (int i = 1; i < 4 * NB; i++) top = fmaxf(top, t[i]);
-            if constexpr (TYPE != SQP_FP16) {
-#pragma unroll
-                for (int i = 0; i < 4 * NB; i++) vmax = fmaxf(vmax, __builtin_fabsf(vs[i >> 2][i & 3]));
+            for (int i = 0; i < 4 * NB; i++) {
+                if constexpr (TYPE == SQP_FP16) {
+                    top = fmaxf(top, t[i]);
+                } else {
+                    const float scale = vs[i >> 2][i & 3];
+                    top = fmaxf(top, t[i] + sqp_log_scale(scale));
+                    vs[i >> 2][i & 3] = sqp_known_scale(scale);
+                }
             }
-            // p 2^-lv times a value's scale stays below 2^15: inside fp16's range, with the running
-            // maximum (in which lv, the logarithm of the largest scale, is counted) changed only now and then.
-            if (__any(top + lv > m + 15.f || (TYPE != SQP_FP16 && vmax > sqp_exp2(lv)))) {
+            if (__any(top > m + 15.f)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                if constexpr (TYPE != SQP_FP16) {
-                    vmax = fmaxf(vmax, __shfl_xor(vmax, 16, 64));
-                    vmax = fmaxf(vmax, __shfl_xor(vmax, 32, 64));
-                    lv = fmaxf(lv, ceilf(__builtin_amdgcn_logf(vmax)));
-                }
-                const float next = top + lv > m + 15.f ? top + lv : m, keep = sqp_exp2(m - next);
+                const float next = top > m + 15.f ? top : m, keep = sqp_exp2(m - next);
                 m = next;
                 l *= keep;
 #pragma unroll
@@ -208,7 +206,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
 #pragma unroll
             for (int d = 0; d < DPL; d++) s_o[wave][col][DPL * (4 * g + r) + d] = o[d][r];
         // A value that is infinite or NaN makes NaN of the rows that do not see it too (zero times it), or of an infinity (times the
-        // two parts of p): then the rows are computed one by one.
+        // two parts of p), and so does one whose scale is negative or large: then the rows are computed one by one.
         f32x4 all = o[0];
 #pragma unroll
         for (int d = 1; d < DPL; d++) all += o[d];  // (finite ones stay far below the largest float)

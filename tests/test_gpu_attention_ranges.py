@@ -1,0 +1,94 @@
+"""GPU parity of the attention over the paged cache where weights and values span a wide range: against 64 bits, with a bound
+in which a token's share is that of its own weight."""
+import pytest
+import torch
+
+import layer_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sqp():
+    import paper_2312_03788_amd as m
+    m.lib()
+    return m
+
+
+def expected(step, floor):
+    """(out, tolerance) [T, heads, D] in 64 bits.  With w_j what is rounded for the matrix cores (p_j, for codes p_j times the value's
+    scale), c_j the value over that scale and A = sum_j p_j |v_j|, the outputs are off by at most
+      output's rounding   2^-11 |o| + 2^-25
+      w's rounding        sum_j max(eps w_j, floor max_i w_i) |c_j|: eps = 2^-22 up to 16 rows per cached head, 2^-11 above (where
+                          fp16 caches sum the rounded p, so that |o| is added to |c_j|); floor: half of fp16's smallest step, 2^-25, over
+                          the least that the largest w is held at
+      scores              (D + 8) 2^-24 sum_d |q_d k_d| scale, the power of two 2^-21, in tiles of codes 2^-16 for the logarithm
+                          of the value's scale (2^-18 of up to 40 each way) and its inverse: of each p, in numerator and denominator
+      sums                len 2^-24 each."""
+    scale, group = step.D ** -0.5, step.heads // step.kv_heads
+    T = step.q.shape[0]
+    out, tol = torch.zeros((T, step.heads, step.D), dtype=torch.float64), torch.full((T, step.heads, step.D), 2.0 ** -25, dtype=torch.float64)
+    codes = step.v.float()
+    for b, (length, n) in enumerate(zip(step.lens, step.news)):
+        if length == 0:
+            continue
+        few = n * group <= 16
+        k, c = step.rows(b, step.k, step.ks), step.rows(b, codes, None)
+        size = step.rows(b, torch.ones_like(codes[..., :1]), step.vs)[..., 0]
+        for i in range(max(0, n - length), n):
+            m, t = length - n + i + 1, int(step.starts[b]) + i
+            for h in range(step.heads):
+                kh, ch, vs, q = k[h // group, :m], c[h // group, :m], size[h // group, :m], step.q[t, h].double()
+                p = torch.softmax(kh @ q * scale, 0)
+                o, A = (p * vs) @ ch, (p * vs) @ ch.abs()
+                w = p * vs
+                d = torch.maximum((2.0 ** -22 if few else 2.0 ** -11) * w, floor * w.max())
+                e = (step.D + 8) * 2.0 ** -24 * scale * (kh.abs() @ q.abs()) + 2.0 ** -21 + (0 if few or step.kind == "fp16" else 2.0 ** -16)
+                out[t, h] = o
+                tol[t, h] += 2.0 ** -11 * o.abs() + d @ ch.abs() + (d.sum() * o.abs() if not few and step.kind == "fp16" else 0) \
+                    + (e * w) @ ch.abs() + (e @ p) * o.abs() + m * 2.0 ** -23 * A
+    return out, tol
+
+
+def compare(step, got, floor):
+    want, tol = expected(step, floor)
+    err = (got.cpu().double() - want).abs()
+    assert bool((err <= tol).all()), "worst error / tolerance %.3f" % float((err / tol).nan_to_num(nan=1e9).max())
+
+
+def attend(sqp, step, **more):
+    return sqp.paged_attention(**step.gpu(), max_q=max(step.news), max_len=max(step.lens), **more)
+
+
+def set_scores(step, of):
+    """Queries and keys whose score of token t, of every sequence and head, is near of(t) as a power of two: the first dimension alone
+    of the keys, the first of the queries 8."""
+    step.q[..., 0] = 8.0
+    raw = step.k if step.kind == "fp16" else step.k.view(torch.int8)
+    for b, length in enumerate(step.lens):
+        for t in range(length):
+            page, place = int(step.table[b, t // step.page]), t % step.page
+            x = of(t) * 0.6931471805599453 * step.D ** 0.5 / 8.0
+            raw[page, :, place] = 0
+            if step.kind == "fp16":
+                step.k[page, :, place, 0] = x
+            else:
+                raw[page, :, place, 0] = 64 if step.kind == "int8" else 0x38  # (0x38: 1.0)
+                step.ks[page, :, place] = x / (64.0 if step.kind == "int8" else 1.0)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("r", [12, 16, 20, 24, 30])
+@pytest.mark.parametrize("lens,news", [([40], [1]), ([40, 1024], [1, 1]), ([90, 33], [2, 3]), ([300], [40])])
+def test_large_values_that_weigh_nothing(sqp, lens, news, r, kind):
+    """Two tokens' value rows, one seen by all and the newest, lie 2^r above the others while their scores leave them nothing
+    (2^-(r + 24)): the other tokens' weights lose no bits to them."""
+    print("case large values", lens, news, r, kind, flush=True)
+    step = ref.Step(lens, news, 8, 2, 128, 16, kind, seed=60)
+    loud = lambda t: t == 5 or t + 1 in lens
+    set_scores(step, lambda t: -(r + 24.0) if loud(t) else (t * 7 % 5) * 0.25)
+    for b, length in enumerate(lens):
+        for t in range(length):
+            if loud(t):
+                step.vs[int(step.table[b, t // 16]), :, t % 16] *= 2.0 ** r
+    compare(step, attend(sqp, step), 2.0 ** -25)
