@@ -283,10 +283,12 @@ int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages,
  *                   (scratch_bytes: max_len = table_width * page then; max_q = 1 without q_starts).
  *   scratch         of this call alone until its work has run, sqp_paged_attention_scratch_bytes() for the preferred plan;
  *                   smaller or NULL: a plan that fits
- * Scores, softmax and sums are fp32; for the matrix cores p is rounded to fp16 (relative 2^-11), in calls whose max_q makes at most 16
- * rows per cached head (max_q * heads / kv_heads) to a sum of two fp16 numbers (2^-22).  What lies past a sequence's length is not used,
- * whatever it holds; nor does a token that sees less depend on the later ones, be they infinite or NaN.  Page numbers outside the cache,
- * lengths past the table and starts past T are taken as the nearest that is inside.  Deterministic.  B <= 65535. */
+ * Scores, softmax and sums are fp32; for the matrix cores a token's weight (p, for 8-bit caches times its value's scale) is rounded to
+ * fp16, which is off by up to 2^-11 of it or 2^-35 of the row's largest weight, whichever is more; sequences of at most 16 rows per cached
+ * head (new tokens * heads / kv_heads) in calls whose max_q makes no more (or that have more than 8 sequences) take it as a sum of two
+ * fp16 numbers (2^-22 of it, or 2^-35 of the largest).  What lies past a sequence's length is not used, whatever it holds; nor does a
+ * token that sees less depend on the later ones, be they infinite or NaN.  Page numbers outside the cache, lengths past the table and
+ * starts past T are taken as the nearest that is inside.  Deterministic.  B <= 65535. */
 size_t sqp_paged_attention_scratch_bytes(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len);
 int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D, int type, int page, int pages, int table_width, int max_q, int max_len,
                         float scale, const void *q, long q_stride, const void *k_cache, const void *v_cache, const float *k_scales,

@@ -213,8 +213,8 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
             }
             asm volatile("" : "+v"(l));
         };
-        // Masks and the running maximum, once a step's scores are there.  p stays below 2^15, inside fp16's range, with the
-        // maximum changed only now and then: at the first tokens, and where a score outgrows it by 2^15.
+        // Masks and the running maximum, once a step's scores are there (SQP_WEIGHT_TOP: the maximum is changed at the first tokens, and
+        // where a score outgrows it).
         auto settle = [&](f32x16 &x, int base) {
             if (__builtin_expect(base + 32 > wave_least, 0)) {
                 top = -INFINITY;
@@ -227,8 +227,8 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
                 }
             }
             const float reach = CODES ? top : top * a.scale2;
-            if (__builtin_expect(__any(reach > m + 15.f), 0)) {
-                const float both = fmaxf(reach, __shfl_xor(reach, 32, 64)), next = both > m + 15.f ? both : m, keep = sqp_exp2(m - next);
+            if (__builtin_expect(__any(reach > m + SQP_WEIGHT_MOST), 0)) {
+                const float both = fmaxf(reach, __shfl_xor(reach, 32, 64)), next = both > m + SQP_WEIGHT_MOST ? both - SQP_WEIGHT_TOP : m, keep = sqp_exp2(m - next);
                 m = next;
                 l *= keep;
                 l2 *= keep;

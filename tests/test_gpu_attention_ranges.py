@@ -92,3 +92,22 @@ def test_large_values_that_weigh_nothing(sqp, lens, news, r, kind):
             if loud(t):
                 step.vs[int(step.table[b, t // 16]), :, t % 16] *= 2.0 ** r
     compare(step, attend(sqp, step), 2.0 ** -25)
+
+
+@pytest.mark.parametrize("kind", ["fp16", "int8", "e4m3"])
+@pytest.mark.parametrize("down", [14, 20, 26])
+@pytest.mark.parametrize("lens,news", [([3000], [1]), ([700, 5000], [1, 2]), ([2500], [20])])
+def test_a_first_token_that_outweighs_a_long_tail(sqp, lens, news, down, kind):
+    """The first token has a score `down` powers of two above all the others and values of zero: the output is the tail's, whose
+    weights are held to 2^-11 (few rows: 2^-22) of themselves or 2^-35 of the largest."""
+    print("case long tail", lens, news, down, kind, flush=True)
+    step = ref.Step(lens, news, 4, 2, 128, 16, kind, seed=61)
+    set_scores(step, lambda t: 0.0 if t == 0 else -down + (t * 7 % 5) * 0.25)
+    if kind == "fp16":
+        step.v.abs_().mul_(50.0)
+    else:
+        step.v.view(torch.uint8).copy_(step.v.float().abs().to(step.v.dtype).view(torch.uint8))
+        step.vs.mul_(50.0)
+    for b in range(len(lens)):
+        step.v.view(torch.int16 if kind == "fp16" else torch.uint8)[int(step.table[b, 0]), :, 0] = 0
+    compare(step, attend(sqp, step), 2.0 ** -35)
