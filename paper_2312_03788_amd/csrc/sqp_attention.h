@@ -380,7 +380,7 @@ __device__ __forceinline__ SqpTile sqp_pick_tile(const SqpAttention &a, int abov
     auto above = [&](int x) {  // tiles of this lane's sequence with a key greater than x
         return len <= x ? 0 : min(n, ((len - x - 1) >> shift) + 1);
     };
-    int lo = -(int)((unsigned)a.T << 1) - 1, hi = a.table_width << a.page_shift;  // no key beyond hi, all above lo
+    int lo = -(all << shift) - 1, hi = a.table_width << a.page_shift;  // no key beyond hi, all above lo (a sequence has at most `all` tiles)
     while (lo < hi) {
         const int mid = lo + ((hi - lo) >> 1);
         if (sqp_wave_sum(above(mid)) <= rank) hi = mid;

@@ -37,16 +37,17 @@ def expected(step, floor):
         size = step.rows(b, torch.ones_like(codes[..., :1]), step.vs)[..., 0]
         for i in range(max(0, n - length), n):
             m, t = length - n + i + 1, int(step.starts[b]) + i
-            for h in range(step.heads):
-                kh, ch, vs, q = k[h // group, :m], c[h // group, :m], size[h // group, :m], step.q[t, h].double()
-                p = torch.softmax(kh @ q * scale, 0)
-                o, A = (p * vs) @ ch, (p * vs) @ ch.abs()
+            for h in range(step.kv_heads):
+                at = slice(h * group, (h + 1) * group)
+                kh, ch, vs, q = k[h, :m], c[h, :m], size[h, :m], step.q[t, at].double()
+                p = torch.softmax(q @ kh.T * scale, 1)
                 w = p * vs
-                d = torch.maximum((2.0 ** -22 if few else 2.0 ** -11) * w, floor * w.max())
-                e = (step.D + 8) * 2.0 ** -24 * scale * (kh.abs() @ q.abs()) + 2.0 ** -21 + (0 if few or step.kind == "fp16" else 2.0 ** -16)
-                out[t, h] = o
-                tol[t, h] += 2.0 ** -11 * o.abs() + d @ ch.abs() + (d.sum() * o.abs() if not few and step.kind == "fp16" else 0) \
-                    + (e * w) @ ch.abs() + (e @ p) * o.abs() + m * 2.0 ** -23 * A
+                o, A = w @ ch, w @ ch.abs()
+                d = torch.maximum((2.0 ** -22 if few else 2.0 ** -11) * w, floor * w.amax(1, keepdim=True))
+                e = (step.D + 8) * 2.0 ** -24 * scale * (q.abs() @ kh.abs().T) + 2.0 ** -21 + (0 if few or step.kind == "fp16" else 2.0 ** -16)
+                out[t, at] = o
+                tol[t, at] += 2.0 ** -11 * o.abs() + d @ ch.abs() + (d.sum(1, keepdim=True) * o.abs() if not few and step.kind == "fp16" else 0) \
+                    + (e * w) @ ch.abs() + (e * p).sum(1, keepdim=True) * o.abs() + m * 2.0 ** -23 * A
     return out, tol
 
 
@@ -111,3 +112,13 @@ def test_a_first_token_that_outweighs_a_long_tail(sqp, lens, news, down, kind):
     for b in range(len(lens)):
         step.v.view(torch.int16 if kind == "fp16" else torch.uint8)[int(step.table[b, 0]), :, 0] = 0
     compare(step, attend(sqp, step), 2.0 ** -35)
+
+
+@pytest.mark.parametrize("lens,news,heads", [([33, 0], [32, 1], 512), ([40, 40], [40, 40], 1024), ([9, 1, 5], [9, 1, 3], 600), ([70, 3], [64, 3], 300)])
+def test_many_query_heads_on_one_cached_head(sqp, lens, news, heads):
+    """More query heads per cached one than a tile has rows, so that a token takes several tiles: every row of several sequences is
+    written (the output holds NaN before)."""
+    print("case many heads", lens, news, heads, flush=True)
+    step = ref.Step(lens, news, heads, 1, 64, 16, "fp16", seed=62)
+    out = torch.full(step.q.shape, float("nan"), dtype=torch.float16, device="cuda")
+    compare(step, attend(sqp, step, out=out), 2.0 ** -35)
