@@ -274,7 +274,8 @@ int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages,
  *   out[t][h] = sum_j p_j v_j,  p = softmax_j (scale q[t][h] . k_j),  h reading the cached head h / (heads / kv_heads)
  * Sequence b has seq_lens[b] cached tokens, token j in page page_table[b][j / page]; its new tokens are the rows
  * q_starts[b] .. q_starts[b + 1] - 1 of q (q_starts [B + 1], not decreasing; NULL: T == B, one token each).  The i-th of its n
- * new tokens sees the tokens j <= seq_lens[b] - n + i.  A token that sees nothing, or belongs to no sequence, gets zeros.
+ * new tokens sees the tokens j <= seq_lens[b] - n + i.  A token that sees nothing, all of whose scores are minus infinity, or that
+ * belongs to no sequence, gets zeros.
  *   q [T][heads][D] fp16, q_stride elements between tokens; out [T][heads][D] fp16
  *   page_table [B][table_width] int32, table_width * page <= 2^30, table_stride entries between rows; entries past a
  *                   sequence's length may be anything

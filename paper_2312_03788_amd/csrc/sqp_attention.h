@@ -269,7 +269,8 @@ __device__ __forceinline__ void sqp_attend_row(const SqpAttention &a, const h16 
                 if constexpr (PER == 2) o[1] += pj * (float)x.y;
             }
         }
-        if (__all(o[0] != o[0] && o[PER - 1] != o[PER - 1])) break;  // NaN as a whole, whatever follows
+        if (l != 0.f && __all(o[0] != o[0] && o[PER - 1] != o[PER - 1])) break;  // NaN as a whole, whatever follows (a sum of zero would
+                                                                                 // make zeros of it: a row all of whose scores are minus infinity)
     }
 }
 

@@ -122,3 +122,17 @@ def test_many_query_heads_on_one_cached_head(sqp, lens, news, heads):
     step = ref.Step(lens, news, heads, 1, 64, 16, "fp16", seed=62)
     out = torch.full(step.q.shape, float("nan"), dtype=torch.float16, device="cuda")
     compare(step, attend(sqp, step, out=out), 2.0 ** -35)
+
+
+@pytest.mark.parametrize("lens,news", [([150], [1]), ([150, 900], [1, 1]), ([300], [40])])
+def test_not_a_number_among_scores_of_minus_infinity(sqp, lens, news):
+    """The first 70 tokens have scores of minus infinity, one of them a value row of NaN: zero times it is NaN, for every row that sees it,
+    whether or not anything has a weight before it."""
+    print("case NaN behind minus infinity", lens, news, flush=True)
+    step = ref.Step(lens, news, 8, 2, 128, 16, "fp16", seed=63)
+    set_scores(step, lambda t: 0.0)
+    for b in range(len(lens)):
+        for t in range(70):
+            step.k[int(step.table[b, t // 16]), :, t % 16, 0] = float("-inf")
+        step.v[int(step.table[b, 1]), :, 3] = float("nan")
+    assert bool(attend(sqp, step).isnan().all())
