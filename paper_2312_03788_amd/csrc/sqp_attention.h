@@ -55,13 +55,14 @@ constexpr float SQP_WEIGHT_TOP = 10.f, SQP_WEIGHT_MOST = 15.9f;
 __device__ __forceinline__ float sqp_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A value's scale in the exponent of its token's weight: its logarithm, of 2^-40 at least (any code times that is below half of
-// fp16's smallest number), so that a token of tiny or zero values keeps its place in the sum of the weights.
-__device__ __forceinline__ float sqp_log_scale(float scale) { return __builtin_amdgcn_logf(fmaxf(scale, 0x1p-40f)); }
-
-// NaN for a scale that the exponent does not take, negative or from 2^40 on (or NaN): it shows in the sums, and leads to the slow way.
-__device__ __forceinline__ float sqp_known_scale(float scale)
+// fp16's smallest number), so that a token of tiny or zero values keeps its place in the sum of the weights (with 2^-100 it lost
+// it beside a weight times scale 2^26 above: fp32's exponents end there).  Others than 0 to 2^40, negative ones and NaN among them, are
+// NaN here: they show in the sums, and lead to the slow way.
+constexpr float SQP_LEAST_SCALE = 0x1p-40f;
+__device__ __forceinline__ bool sqp_known_scale(float scale) { return __builtin_bit_cast(uint32_t, scale) < 0x53800000u; }  // (the bits of 2^40)
+__device__ __forceinline__ float sqp_log_scale(float scale)
 {
-    return __builtin_bit_cast(uint32_t, scale) < 0x53800000u ? scale : __builtin_nanf("");
+    return sqp_known_scale(scale) ? __builtin_amdgcn_logf(fmaxf(scale, SQP_LEAST_SCALE)) : __builtin_nanf("");
 }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                 } else {
                     const float scale = vs[i >> 2][i & 3];
                     top = fmaxf(top, t[i] + sqp_log_scale(scale));
-                    vs[i >> 2][i & 3] = sqp_known_scale(scale);
+                    if (!sqp_known_scale(scale)) vs[i >> 2][i & 3] = __builtin_nanf("");
                 }
             }
             if (__any(top > m + SQP_WEIGHT_MOST)) {

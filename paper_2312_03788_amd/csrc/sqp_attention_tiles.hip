@@ -129,8 +129,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
                 *(h16x8 *)&to[16 * (unit % KU) + 8 * (piece & 1)] = h16x8{p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
                 if (piece == KPIECES - 1 && lane < TOKENS) {
                     s_ks[buf][16 * block16 + first_token + lane] = kscale * a.scale2;
-                    const float x = fmaxf(kvscale, 0x1p-100f);
-                    s_lv[buf][16 * block16 + first_token + lane] = kvscale >= 0.f ? __builtin_amdgcn_logf(x) : __builtin_nanf("");
+                    s_lv[buf][16 * block16 + first_token + lane] = sqp_log_scale(kvscale);
                 }
             } else {
                 *(u32x4 *)&to[8 * (unit % KU)] = u32x4{kw[4 * i], kw[4 * i + 1], kw[4 * i + 2], kw[4 * i + 3]};
@@ -154,7 +153,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
 #pragma unroll
             for (int j = 0; j < 4; j++) x[j] = sqp_pair<TYPE>(&vw[2 * j * VW], &vw[(2 * j + 1) * VW], d);
             *(u32x4 *)&s_v[buf][(32 * VSUB * d + v_lane) * VROW + 16 * block16 + 8 * v_half] = x;
-            if (CODES && d == VD - 1 && lane < TOKENS) s_rv[buf][16 * block16 + first_token + lane] = 1.f / fmaxf(vscale, 0x1p-100f);
+            if (CODES && d == VD - 1 && lane < TOKENS) s_rv[buf][16 * block16 + first_token + lane] = 1.f / fmaxf(vscale, SQP_LEAST_SCALE);
         };
 
         // ---- steps
@@ -368,7 +367,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         l += l2;
         l += __shfl_xor(l, 32, 64);
         // A value that is infinite or NaN makes NaN of the rows that do not see it too (zero times it), and so does one whose p
-        // is too small for fp16, and any whose scale is negative: then the wave's rows are computed one by one.
+        // is too small for fp16, and any whose scale is negative or large: then the wave's rows are computed one by one.
         float all = 0.f;
 #pragma unroll
         for (int d = 0; d < NV; d++) {

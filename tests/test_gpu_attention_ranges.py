@@ -136,3 +136,36 @@ def test_not_a_number_among_scores_of_minus_infinity(sqp, lens, news):
             step.k[int(step.table[b, t // 16]), :, t % 16, 0] = float("-inf")
         step.v[int(step.table[b, 1]), :, 3] = float("nan")
     assert bool(attend(sqp, step).isnan().all())
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("lens,news", [([12000], [1]), ([12000], [20]), ([90, 12000], [33, 20])])
+def test_tokens_of_zero_values_keep_their_weight(sqp, lens, news, kind):
+    """One token with a weight 2^20 above the others' and large values, thousands of zero values (scale 0): these have 1 % of the
+    sum, in whatever part of the sequence they are."""
+    print("case zero values", lens, news, kind, flush=True)
+    step = ref.Step(lens, news, 4, 2, 128, 16, kind, seed=64)
+    set_scores(step, lambda t: 20.0 if t == 5 else 0.0)
+    for b, length in enumerate(lens):
+        for t in range(length):
+            step.vs[int(step.table[b, t // 16]), :, t % 16] = (2.0 ** 9 if kind == "int8" else 2.0 ** 7) if t == 5 else 0.0
+    compare(step, attend(sqp, step), 2.0 ** -35)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("n", [1, 40])
+def test_value_scales_up_to_large_powers(sqp, n, kind):
+    """Value scales of 2^-60 to 2^60 beside each other, with scores that leave the large ones a share of the output or more: outputs inside
+    fp16's range are to 64 bits, the others are infinite with the right sign."""
+    print("case large scales", n, kind, flush=True)
+    step = ref.Step([300], [n], 8, 2, 128, 16, kind, seed=65)
+    power = lambda t: t * 41 % 121 - 60
+    set_scores(step, lambda t: -1.0 * max(power(t) - (16 if t % 7 == 0 else 0), 0))
+    for t in range(300):
+        step.vs[int(step.table[0, t // 16]), :, t % 16] = 2.0 ** power(t)
+    got = attend(sqp, step).cpu().double()
+    want, tol = expected(step, 2.0 ** -35)
+    top = 65520.0  # (from here on rounding gives an infinity)
+    inside, outside = want.abs() < 65504.0 - tol, want.abs() > top + tol
+    assert bool(inside.any()) and bool(((got - want).abs() <= tol)[inside].all())
+    assert bool((got == torch.sign(want) * float("inf"))[outside].all())
