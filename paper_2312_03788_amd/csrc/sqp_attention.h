@@ -21,10 +21,10 @@ struct SqpAttention {
 
 // A long sequence is read in parts of `chunk` tokens by workgroups of their own (at most `parts` of them, the last one takes
 // what is left).  A row that sees one part only is written at once; of the others every part leaves its maximum, sum and
-// output, which sqp_attention_combine joins.  A partial result is D + 4 floats: the output, the maximum, the sum.
+// output, which sqp_attention_combine joins.  A partial result is D + 4 floats: the output, the maximum, the sum; a row has
+// `parts` of them, at its slot.
 struct SqpParts {
     int chunk, parts;
-    int pitch;      // partial results per row
     float *part;
     __host__ __device__ int of(int sees) const
     {
@@ -38,7 +38,9 @@ struct SqpParts {
 // kernel those of up to `most_rows` rows, the tile kernel those of more than `above_rows`.
 constexpr int SQP_FEW_ROWS = 16;
 
-void sqp_attention_few(int type, int D, const SqpAttention &a, const SqpParts &p, int most_rows, hipStream_t stream);
+// Slots: the tile kernel's rows have them in the order of the output; the few-rows kernel has `slots` for every sequence and cached
+// head (a sequence of more rows than that is not split), so that they cost what its rows need and not all rows of a prompt beside them.
+void sqp_attention_few(int type, int D, const SqpAttention &a, const SqpParts &p, int most_rows, int slots, hipStream_t stream);
 void sqp_attention_tiles(int type, int D, const SqpAttention &a, const SqpParts &p, int tile_rows, int above_rows, int fold, hipStream_t stream);
 
 #ifdef __HIPCC__
@@ -188,12 +190,12 @@ __device__ __forceinline__ size_t sqp_cache_row(const SqpAttention &a, const int
     return (block << a.page_shift) + (token & ((1 << a.page_shift) - 1));
 }
 
-// Where a row's result of one part goes; false: this part has nothing of the row.
+// Where a row's result of one part goes (null: the output); false: this part has nothing of the row.
 template <int D>
-__device__ __forceinline__ bool sqp_target(const SqpParts &p, int sees, int part, long row, float *&partial)
+__device__ __forceinline__ bool sqp_target(const SqpParts &p, int sees, int part, long slot, float *&partial)
 {
     const int n = p.of(sees);
-    partial = n > 1 ? p.part + ((size_t)row * p.pitch + part) * (D + 4) : nullptr;
+    partial = n > 1 ? p.part + ((size_t)slot * p.parts + part) * (D + 4) : nullptr;
     return part < n;
 }
 
@@ -278,13 +280,13 @@ __device__ __forceinline__ void sqp_attend_row(const SqpAttention &a, const h16 
 // The same for a row of a part, result included: the slow way of the kernels below where a value is infinite or NaN (zero times
 // it is not zero, so the matrix instructions cannot keep it from the rows that do not see it).
 template <int TYPE, int D>
-__device__ __forceinline__ void sqp_attend_row_of_part(const SqpAttention &a, const SqpParts &parts, int part, int token, int head, int sees, const int *table_row, int lo,
-                                                       int hi)
+__device__ __forceinline__ void sqp_attend_row_of_part(const SqpAttention &a, const SqpParts &parts, int part, long slot, int token, int head, int sees,
+                                                       const int *table_row, int lo, int hi)
 {
     constexpr int PER = D / 64;
     const long row = (long)token * a.heads + head;
     float *partial, m, l, o[PER];
-    if (!sqp_target<D>(parts, sees, part, row, partial)) return;
+    if (!sqp_target<D>(parts, sees, part, slot, partial)) return;
     sqp_attend_row<TYPE, D>(a, a.q + token * a.q_stride + head * D, table_row, head / a.group, lo, min(hi, sees), m, l, o);
     const int lane = threadIdx.x & 63;
 #pragma unroll

@@ -9,27 +9,45 @@ int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const vo
 
 namespace {
 
-// Joins the parts of the rows that have more than one: a wave per row, a lane per part for the weights; then D / 4 lanes have four
-// values of a part each, so that two (D = 128) or four parts are read at once.
+// Joins the parts of the rows that have more than one: a wave per slot (the few-rows kernel's `few_slots`, then the tile kernel's),
+// a lane per part for the weights; then D / 4 lanes have four values of a part each, so that two (D = 128) or four parts are read at
+// once.
 template <int D>
-__global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttention a, const SqpParts few, const SqpParts tiles, int most_rows)
+__global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttention a, const SqpParts few, const SqpParts tiles, int most_rows, int slots,
+                                                                int few_slots, int all_slots)
 {
     constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
-    const int row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));  // (T heads D < 2^31)
-    if (row >= a.T * a.heads) return;
-    const int lane = threadIdx.x & 63, token = row / a.heads, d = 4 * (lane % LANES), which = lane / LANES;
+    const int at = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    if (at >= all_slots) return;
+    const bool is_few = at < few_slots;
+    const int slot = is_few ? at : at - few_slots;
+    const SqpParts &p = is_few ? few : tiles;
+    const int lane = threadIdx.x & 63, d = 4 * (lane % LANES), which = lane / LANES;
     // read before it is known how many parts there are: the chain of loads is what this kernel takes
-    const int pitch = few.pitch;
-    const float *part = few.part + (size_t)row * pitch * (D + 4);
-    const float m0 = part[min(lane, pitch - 1) * (D + 4) + D], l0 = part[min(lane, pitch - 1) * (D + 4) + D + 1];
+    const float *part = p.part + (size_t)slot * p.parts * (D + 4);
+    const float m0 = part[min(lane, p.parts - 1) * (D + 4) + D], l0 = part[min(lane, p.parts - 1) * (D + 4) + D + 1];
     f32x4 x[4];
 #pragma unroll
-    for (int j = 0; j < 4; j++) x[j] = *(const f32x4 *)&part[min(j * AT_ONCE + which, pitch - 1) * (D + 4) + d];
-    const int b = __builtin_amdgcn_readfirstlane(sqp_sequence_of(a, token));
-    if (b >= a.B) return;
-    const SqpSequence s = sqp_one_sequence(a, b);
-    const SqpParts &p = s.n * a.group <= most_rows ? few : tiles;
-    const int n = p.of(s.len - s.n + (token - s.first) + 1);
+    for (int j = 0; j < 4; j++) x[j] = *(const f32x4 *)&part[min(j * AT_ONCE + which, p.parts - 1) * (D + 4) + d];
+    int b, row, sees;
+    if (is_few) {
+        const int kv_head = slot / slots % a.kv_heads, r = slot % slots, token = r / a.group;
+        b = slot / (a.kv_heads * slots);
+        const SqpSequence s = sqp_one_sequence(a, b);
+        const int rows = s.n * a.group;
+        if (r >= rows || rows > slots || rows > most_rows) return;
+        row = (s.first + token) * a.heads + kv_head * a.group + r - token * a.group;  // (T heads D < 2^31)
+        sees = s.len - s.n + token + 1;
+    } else {
+        const int token = slot / a.heads;
+        row = slot;
+        b = __builtin_amdgcn_readfirstlane(sqp_sequence_of(a, token));
+        if (b >= a.B) return;
+        const SqpSequence s = sqp_one_sequence(a, b);
+        if (s.n * a.group <= most_rows) return;
+        sees = s.len - s.n + (token - s.first) + 1;
+    }
+    const int n = p.of(sees);
     if (n == 1) return;
     const float m = lane < n ? m0 : SQP_LOWEST;
     const float top = sqp_wave_join<true>(m);
@@ -43,9 +61,9 @@ __global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttenti
         }
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-            const int at = i + j * AT_ONCE + which;
-            const float wj = __shfl(w, at & 63, 64);
-            if (at < n) o += wj * x[j];
+            const int from = i + j * AT_ONCE + which;
+            const float wj = __shfl(w, from & 63, 64);
+            if (from < n) o += wj * x[j];
         }
     }
 #pragma unroll
@@ -64,7 +82,9 @@ __global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttenti
 struct Plan {
     bool few, tiles;    // which kernels
     int tile_rows;      // 128 or 256
-    SqpParts f, t;      // their parts (pitch: of both, 1 if nothing is split)
+    SqpParts f, t;      // their parts
+    int slots;          // of the few-rows kernel, per sequence and cached head
+    int few_slots, tile_slots;  // of rows that may have more than one part
     int fold;           // tiles on the first half of the places, the shortest then share theirs (0: none)
     size_t bytes;       // of partial results
 };
@@ -106,16 +126,19 @@ Plan plan(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len, 
     p.t = split(blocks, 512, 512, max_len, most_parts);
     const int at_once = p.tile_rows == 128 ? 512 : 256;
     p.fold = blocks * p.t.parts <= at_once && p.tile_rows == 128 ? 256 / (kv_heads * p.t.parts) : 0;
-    const int pitch = std::max(p.few ? p.f.parts : 1, p.tiles ? p.t.parts : 1);
-    p.f.pitch = p.t.pitch = pitch;
-    p.bytes = pitch > 1 ? (size_t)T * heads * pitch * (D + 4) * sizeof(float) : 0;
+    // (Parts are only made of few groups: at most 256 of a sequence and cached head, or of tiles, so the slots are few as well.)
+    p.slots = p.tiles ? SQP_FEW_ROWS : (int)rows;
+    p.few_slots = p.few && p.f.parts > 1 ? B * kv_heads * p.slots : 0;
+    p.tile_slots = p.tiles && p.t.parts > 1 ? T * heads : 0;
+    p.bytes = ((size_t)p.few_slots * p.f.parts + (size_t)p.tile_slots * p.t.parts) * (D + 4) * sizeof(float);
     return p;
 }
 
 template <int D>
 void combine(const SqpAttention &a, const Plan &p, int most_rows, hipStream_t st)
 {
-    attention_combine_kernel<D><<<(unsigned)((a.T * a.heads + 3) / 4), 256, 0, st>>>(a, p.f, p.t, most_rows);
+    const int all = p.few_slots + p.tile_slots;
+    attention_combine_kernel<D><<<(unsigned)((all + 3) / 4), 256, 0, st>>>(a, p.f, p.t, most_rows, p.slots, p.few_slots, all);
 }
 
 }  // namespace
@@ -152,14 +175,14 @@ extern "C" int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D,
     a.scale2 = scale * 1.44269504088896340736f;
     hipStream_t st = (hipStream_t)stream;
     const int reach = max_len > 0 ? max_len : table_width * page, most_q = q_starts ? max_q : 1;
-    const size_t row_bytes = (size_t)T * heads * (D + 4) * sizeof(float);
     Plan p = plan(T, B, heads, kv_heads, D, most_q, reach, MOST_PARTS);
-    if (p.bytes > (scratch ? scratch_bytes : 0))
-        p = plan(T, B, heads, kv_heads, D, most_q, reach, scratch ? (int)std::max((size_t)1, scratch_bytes / row_bytes) : 1);
-    p.f.part = p.t.part = (float *)scratch;
+    const size_t room = scratch ? scratch_bytes : 0;
+    for (int most = room ? MOST_PARTS - 1 : 1; p.bytes > room; most--) p = plan(T, B, heads, kv_heads, D, most_q, reach, most);  // (one part takes none)
+    p.f.part = (float *)scratch;
+    p.t.part = p.f.part + (size_t)p.few_slots * p.f.parts * (D + 4);
     const int most_rows = !p.few ? -1 : !p.tiles ? INT_MAX : SQP_FEW_ROWS;  // of the few-rows kernel
-    if (p.few) sqp_attention_few(type, D, a, p.f, most_rows, st);
+    if (p.few) sqp_attention_few(type, D, a, p.f, most_rows, p.slots, st);
     if (p.tiles) sqp_attention_tiles(type, D, a, p.t, p.tile_rows, std::max(most_rows, 0), p.fold, st);
-    if (p.f.pitch > 1) D == 128 ? combine<128>(a, p, most_rows, st) : combine<64>(a, p, most_rows, st);
+    if (p.few_slots + p.tile_slots > 0) D == 128 ? combine<128>(a, p, most_rows, st) : combine<64>(a, p, most_rows, st);
     return sqp_launch_status();
 }

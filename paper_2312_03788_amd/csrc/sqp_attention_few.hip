@@ -25,7 +25,7 @@
 namespace {
 
 template <int TYPE, int D>
-__global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttention a, const SqpParts parts, int most_rows)
+__global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttention a, SqpParts parts, int most_rows, int slots)
 {
     constexpr int BYTES = SqpCode<TYPE>::BYTES;
     constexpr int KL = D * BYTES / 64;       // 16-byte loads per lane and 16 keys
@@ -42,6 +42,8 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
     const SqpSequence s = sqp_one_sequence(a, b);
     const int rows = s.n * a.group;
     if (rows > most_rows) return;
+    if (rows > slots) parts.parts = 1;
+    const long first_slot = ((long)b * a.kv_heads + kv_head) * slots;
     const int *table = a.table + b * a.table_stride;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
     const int before = s.len - s.n;  // token i of the new ones sees before + i + 1
@@ -216,14 +218,14 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
         if (s_bad) {
             for (int r = row0 + wave; r < row0 + count; r += 4) {
                 const int tk = r / a.group;
-                sqp_attend_row_of_part<TYPE, D>(a, parts, part, s.first + tk, kv_head * a.group + r - tk * a.group, before + tk + 1, table, lo, hi);
+                sqp_attend_row_of_part<TYPE, D>(a, parts, part, first_slot + r, s.first + tk, kv_head * a.group + r - tk * a.group, before + tk + 1, table, lo, hi);
             }
         }
         for (int i = s_bad ? count * (D / 4) : (int)threadIdx.x; i < count * (D / 4); i += 256) {
             const int r = i / (D / 4), d = 4 * (i % (D / 4)), tk = (row0 + r) / a.group;
             const long at = (long)(s.first + tk) * a.heads + kv_head * a.group + row0 + r - tk * a.group;
             float *partial;
-            if (!sqp_target<D>(parts, before + tk + 1, part, at, partial)) continue;
+            if (!sqp_target<D>(parts, before + tk + 1, part, first_slot + row0 + r, partial)) continue;
             const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
             float sum = 0.f;
             f32x4 x = (f32x4)(0.f);
@@ -252,16 +254,16 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
 }
 
 template <int TYPE, int D>
-void launch(const SqpAttention &a, const SqpParts &p, int most_rows, hipStream_t st)
+void launch(const SqpAttention &a, const SqpParts &p, int most_rows, int slots, hipStream_t st)
 {
-    attention_few_kernel<TYPE, D><<<dim3((unsigned)a.kv_heads, (unsigned)a.B, (unsigned)p.parts), 256, 0, st>>>(a, p, most_rows);
+    attention_few_kernel<TYPE, D><<<dim3((unsigned)a.kv_heads, (unsigned)a.B, (unsigned)p.parts), 256, 0, st>>>(a, p, most_rows, slots);
 }
 
 }  // namespace
 
-void sqp_attention_few(int type, int D, const SqpAttention &a, const SqpParts &p, int most_rows, hipStream_t st)
+void sqp_attention_few(int type, int D, const SqpAttention &a, const SqpParts &p, int most_rows, int slots, hipStream_t st)
 {
-#define FEW(TYPE) (D == 128 ? launch<TYPE, 128>(a, p, most_rows, st) : launch<TYPE, 64>(a, p, most_rows, st))
+#define FEW(TYPE) (D == 128 ? launch<TYPE, 128>(a, p, most_rows, slots, st) : launch<TYPE, 64>(a, p, most_rows, slots, st))
     if (type == SQP_FP16) FEW(SQP_FP16);
     else if (type == SQP_INT8) FEW(SQP_INT8);
     else FEW(SQP_E4M3);

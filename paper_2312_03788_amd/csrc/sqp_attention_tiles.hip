@@ -378,8 +378,8 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         }
         if (__any(!(__builtin_fabsf(all) < INFINITY))) {
             for (int r = wave_row; r <= min(wave_row + 31, row_last); r++) {
-                const int tk = r / a.group;
-                sqp_attend_row_of_part<TYPE, D>(a, parts, part, s.first + tk, kv_head * a.group + r - tk * a.group, before + tk + 1, table, lo, hi);
+                const int tk = r / a.group, hd = kv_head * a.group + r - tk * a.group;
+                sqp_attend_row_of_part<TYPE, D>(a, parts, part, (long)(s.first + tk) * a.heads + hd, s.first + tk, hd, before + tk + 1, table, lo, hi);
             }
         } else if (row0 + 32 * wave + col < rows) {
             const long at = (long)(s.first + token) * a.heads + head;
