@@ -257,8 +257,8 @@ int sqp_add_rmsnorm_quant(int M, int H, int type, const void *x, const void *res
  *
  * Writes the keys and values of T tokens into their slots; on the way keys, and queries if there are any, are rotated:
  *   y[j] = x[j] c[j] - x[D/2 + j] s[j],  y[D/2 + j] = x[D/2 + j] c[j] + x[j] s[j],  c | s = cos_sin[position], fp32
- * (cos_sin [n_positions][D] fp32: D/2 cosines, D/2 sines; NULL: no rotation), and keys and values are quantised from these
- * fp32 values.  q [T][heads][D], k, v [T][kv_heads][D] fp16 with the given distances between tokens (elements, multiples of 8),
+ * (cos_sin [n_positions][D] fp32: D/2 cosines, D/2 sines; NULL: no rotation; every product and sum rounded for itself), and keys and
+ * values are quantised from these fp32 values.  q [T][heads][D], k, v [T][kv_heads][D] fp16 with the given distances between tokens (elements, multiples of 8),
  * q_out [T][heads][D] fp16 (heads == 0: no queries, q and q_out unused).  A token whose slot lies outside the cache (-1, say)
  * is not written; one whose position lies outside the table becomes NaN.  Two tokens in one slot: either may end there.
  * T == 0 enqueues nothing. */

@@ -50,6 +50,8 @@ __global__ void __launch_bounds__(256) kv_write_kernel(const CacheArgs a)
                 const float *cs = a.cos_sin + (size_t)pos * D + 8 * lane;
 #pragma unroll
                 for (int j = 0; j < 8; j++) {
+                    // every product and sum rounded for itself: codes at a rounding's edge are those of plain 32-bit arithmetic
+#pragma clang fp contract(off)
                     const float c = cs[j], s = cs[D / 2 + j], x = f[j], y = f[8 + j];
                     f[j] = x * c - y * s;
                     f[8 + j] = y * c + x * s;
