@@ -58,13 +58,16 @@ __device__ __forceinline__ float sqp_exp2(float x) { return __builtin_amdgcn_exp
 
 // A value's scale in the exponent of its token's weight: its logarithm, of 2^-40 at least (any code times that is below half of
 // fp16's smallest number), so that a token of tiny or zero values keeps its place in the sum of the weights (with 2^-100 it lost
-// it beside a weight times scale 2^26 above: fp32's exponents end there).  Others than 0 to 2^40, negative ones and NaN among them, are
-// NaN here: they show in the sums, and lead to the slow way.
+// it beside a weight times scale 2^26 above: fp32's exponents end there).
 constexpr float SQP_LEAST_SCALE = 0x1p-40f;
-__device__ __forceinline__ bool sqp_known_scale(float scale) { return __builtin_bit_cast(uint32_t, scale) < 0x53800000u; }  // (the bits of 2^40)
-__device__ __forceinline__ float sqp_log_scale(float scale)
+__device__ __forceinline__ float sqp_log_scale(float scale) { return __builtin_amdgcn_logf(fmaxf(__builtin_fabsf(scale), SQP_LEAST_SCALE)); }
+
+// A scale of 2^40 or more as NaN, which shows in the sums and leads to the slow way (by arithmetic: with a comparison
+// and its mask per token a decode step of 16 sequences at up to 8192 tokens takes 39.1 us instead of 38.8).
+__device__ __forceinline__ float sqp_known_scale(float scale)
 {
-    return sqp_known_scale(scale) ? __builtin_amdgcn_logf(fmaxf(scale, SQP_LEAST_SCALE)) : __builtin_nanf("");
+    const float far = scale * 0x1p88f;  // infinite then
+    return scale + (far - far);
 }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
     const int rows = s.n * a.group;
     if (rows > most_rows) return;
     if (rows > slots) parts.parts = 1;
-    const long first_slot = ((long)b * a.kv_heads + kv_head) * slots;
+    auto slot = [&](int r) { return ((long)b * a.kv_heads + kv_head) * slots + r; };
     const int *table = a.table + b * a.table_stride;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
     const int before = s.len - s.n;  // token i of the new ones sees before + i + 1
@@ -150,16 +150,15 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             }
             // What goes through the matrix cores is p times the value's scale, so the running maximum is taken of that: t + log2 of
             // the token's own scale (SQP_WEIGHT_TOP: changed only now and then).
-            float top = -INFINITY;
+            float top = 0.f;
 #pragma unroll
             for (int i = 0; i < 4 * NB; i++) {
-                if constexpr (TYPE == SQP_FP16) {
-                    top = fmaxf(top, t[i]);
-                } else {
-                    const float scale = vs[i >> 2][i & 3];
-                    top = fmaxf(top, t[i] + sqp_log_scale(scale));
-                    if (!sqp_known_scale(scale)) vs[i >> 2][i & 3] = __builtin_nanf("");
+                float weight = t[i];
+                if constexpr (TYPE != SQP_FP16) {
+                    weight += sqp_log_scale(vs[i >> 2][i & 3]);
+                    vs[i >> 2][i & 3] = sqp_known_scale(vs[i >> 2][i & 3]);
                 }
+                top = i == 0 ? weight : fmaxf(top, weight);
             }
             if (__any(top > m + SQP_WEIGHT_MOST)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -208,7 +207,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
 #pragma unroll
             for (int d = 0; d < DPL; d++) s_o[wave][col][DPL * (4 * g + r) + d] = o[d][r];
         // A value that is infinite or NaN makes NaN of the rows that do not see it too (zero times it), or of an infinity (times the
-        // two parts of p), and so does one whose scale is negative or large: then the rows are computed one by one.
+        // two parts of p), and so does one whose scale is 2^40 or more: then the rows are computed one by one.
         f32x4 all = o[0];
 #pragma unroll
         for (int d = 1; d < DPL; d++) all += o[d];  // (finite ones stay far below the largest float)
@@ -218,14 +217,14 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
         if (s_bad) {
             for (int r = row0 + wave; r < row0 + count; r += 4) {
                 const int tk = r / a.group;
-                sqp_attend_row_of_part<TYPE, D>(a, parts, part, first_slot + r, s.first + tk, kv_head * a.group + r - tk * a.group, before + tk + 1, table, lo, hi);
+                sqp_attend_row_of_part<TYPE, D>(a, parts, part, slot(r), s.first + tk, kv_head * a.group + r - tk * a.group, before + tk + 1, table, lo, hi);
             }
         }
         for (int i = s_bad ? count * (D / 4) : (int)threadIdx.x; i < count * (D / 4); i += 256) {
             const int r = i / (D / 4), d = 4 * (i % (D / 4)), tk = (row0 + r) / a.group;
             const long at = (long)(s.first + tk) * a.heads + kv_head * a.group + row0 + r - tk * a.group;
             float *partial;
-            if (!sqp_target<D>(parts, before + tk + 1, part, first_slot + row0 + r, partial)) continue;
+            if (!sqp_target<D>(parts, before + tk + 1, part, slot(row0 + r), partial)) continue;
             const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
             float sum = 0.f;
             f32x4 x = (f32x4)(0.f);

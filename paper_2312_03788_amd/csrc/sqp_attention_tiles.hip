@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
                 *(h16x8 *)&to[16 * (unit % KU) + 8 * (piece & 1)] = h16x8{p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
                 if (piece == KPIECES - 1 && lane < TOKENS) {
                     s_ks[buf][16 * block16 + first_token + lane] = kscale * a.scale2;
-                    s_lv[buf][16 * block16 + first_token + lane] = sqp_log_scale(kvscale);
+                    s_lv[buf][16 * block16 + first_token + lane] = kvscale >= 0.f && kvscale < 0x1p40f ? sqp_log_scale(kvscale) : __builtin_nanf("");
                 }
             } else {
                 *(u32x4 *)&to[8 * (unit % KU)] = u32x4{kw[4 * i], kw[4 * i + 1], kw[4 * i + 2], kw[4 * i + 3]};
