@@ -287,7 +287,7 @@ int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages,
  * Scores, softmax and sums are fp32; for the matrix cores a token's weight (p, for 8-bit caches times its value's scale) is rounded to
  * fp16, which is off by up to 2^-11 of it or 2^-35 of the row's largest weight, whichever is more; sequences of at most 16 rows per cached
  * head (new tokens * heads / kv_heads) take it as a sum of two fp16 numbers (2^-22 of it, or 2^-35 of the largest) where max_q makes no
- * more, or is right and there are more than 8 sequences.  What lies past a sequence's length is not used, whatever it holds; nor does a
+ * more; beside longer ones they are rounded in one way or the other.  What lies past a sequence's length is not used, whatever it holds; nor does a
  * token that sees less depend on the later ones, be they infinite or NaN.  Page numbers outside the cache, lengths past the table and
  * starts past T are taken as the nearest that is inside.  Deterministic.  B <= 65535. */
 size_t sqp_paged_attention_scratch_bytes(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len);

@@ -9,19 +9,15 @@ int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const vo
 
 namespace {
 
-// Joins the parts of the rows that have more than one: a wave per slot (the few-rows kernel's `few_slots`, then the tile kernel's),
-// a lane per part for the weights; then D / 4 lanes have four values of a part each, so that two (D = 128) or four parts are read at
-// once.
+// Joins the parts of the rows that have more than one: a wave per slot (the few-rows kernel's, `slots` per sequence and cached head, or
+// with slots == 0 the tile kernel's), a lane per part for the weights; then D / 4 lanes have four values of a part each, so that two
+// (D = 128) or four parts are read at once.
 template <int D>
-__global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttention a, const SqpParts few, const SqpParts tiles, int most_rows, int slots,
-                                                                int few_slots, int all_slots)
+__global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttention a, const SqpParts p, int most_rows, int slots, int all_slots)
 {
     constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
-    const int at = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-    if (at >= all_slots) return;
-    const bool is_few = at < few_slots;
-    const int slot = is_few ? at : at - few_slots;
-    const SqpParts &p = is_few ? few : tiles;
+    const int slot = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    if (slot >= all_slots) return;
     const int lane = threadIdx.x & 63, d = 4 * (lane % LANES), which = lane / LANES;
     // read before it is known how many parts there are: the chain of loads is what this kernel takes
     const float *part = p.part + (size_t)slot * p.parts * (D + 4);
@@ -29,22 +25,19 @@ __global__ void __launch_bounds__(256) attention_combine_kernel(const SqpAttenti
     f32x4 x[4];
 #pragma unroll
     for (int j = 0; j < 4; j++) x[j] = *(const f32x4 *)&part[min(j * AT_ONCE + which, p.parts - 1) * (D + 4) + d];
-    int b, row, sees;
-    if (is_few) {
-        const int kv_head = slot / slots % a.kv_heads, r = slot % slots, token = r / a.group;
-        b = slot / (a.kv_heads * slots);
+    int row, sees;
+    if (slots) {
+        const int b = slot / (a.kv_heads * slots), kv_head = slot / slots % a.kv_heads, r = slot % slots, token = r / a.group;
         const SqpSequence s = sqp_one_sequence(a, b);
         const int rows = s.n * a.group;
         if (r >= rows || rows > slots || rows > most_rows) return;
         row = (s.first + token) * a.heads + kv_head * a.group + r - token * a.group;  // (T heads D < 2^31)
         sees = s.len - s.n + token + 1;
     } else {
-        const int token = slot / a.heads;
-        row = slot;
-        b = __builtin_amdgcn_readfirstlane(sqp_sequence_of(a, token));
+        const int token = slot / a.heads, b = __builtin_amdgcn_readfirstlane(sqp_sequence_of(a, token));
         if (b >= a.B) return;
         const SqpSequence s = sqp_one_sequence(a, b);
-        if (s.n * a.group <= most_rows) return;
+        row = slot;
         sees = s.len - s.n + (token - s.first) + 1;
     }
     const int n = p.of(sees);
@@ -84,7 +77,7 @@ struct Plan {
     int tile_rows;      // 128 or 256
     SqpParts f, t;      // their parts
     int slots;          // of the few-rows kernel, per sequence and cached head
-    int few_slots, tile_slots;  // of rows that may have more than one part
+    int few_slots, tile_slots;  // of rows that may have more than one part: of one kernel at most
     int fold;           // tiles on the first half of the places, the shortest then share theirs (0: none)
     size_t bytes;       // of partial results
 };
@@ -92,9 +85,12 @@ struct Plan {
 constexpr int MOST_PARTS = 64;  // a lane each when they are joined
 
 // Parts: as many as make `wanted` workgroups of these groups, each of at least `least` tokens.  512 workgroups, two per compute unit,
-// are what runs at once: decoding at 8192 (16 sequences, 8 cached heads, e4m3) takes 47 us with parts for 512, 53 with 768, 48.5
-// with 1024, one sequence at 32000 (int8) 82, 89 and 82.  The tile kernel's parts cost their partial results besides (a 2048-token
-// prompt in parts of 1024 takes 92 us instead of 66), so its tiles are only split where they leave half the chip empty.
+// are what runs at once: 16 sequences of up to 8192 tokens (8 cached heads, e4m3) take 38.9 us with parts for 512, 41.3 with 768, 40.8
+// with 1024; one of 32000 (40 cached heads, int8) 67.1, 67.2, 66.4; 33 of up to 1570 (8 cached heads, int8) 25.4, 25.4, 23.4; 43 of up to
+// 5152 (one cached head, int8) 18.3, 17.2, 19.0.  Where max_len is far above the lengths more would be better: one sequence of 2048 tokens,
+// 32 heads, takes 9.8 us with its own length as max_len and 25.1, 20.4, 16.8 with 32768.  The tile kernel's parts cost their partial
+// results besides, so its tiles are only split where they leave half the chip empty: wanting 1024, a 2048-token prompt takes 84.9 us
+// instead of 65.2, a mixed step of six sequences 199 instead of 156.
 SqpParts split(long groups, long wanted, int least, int max_len, int most_parts)
 {
     const long parts = std::max(1L, std::min((long)most_parts, wanted / std::max(groups, 1L)));
@@ -112,21 +108,28 @@ Plan plan(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len, 
     max_q = std::max(1, std::min(max_q > 0 ? max_q : T, T));
     max_len = std::max(max_len, 1);
     const long rows = (long)max_q * group;
-    // Single tokens beside prompts: the few-rows kernel reads their cache faster, but its launch waits for the other one's end. Up to
-    // 8 sequences the tile kernel takes them along (four prompts and two tokens of 64 heads on 8: 194 -> 171 us).
-    p.few = rows <= SQP_FEW_ROWS || (group <= SQP_FEW_ROWS && (long)B * max_q > T && B > 8);
-    p.tiles = rows > SQP_FEW_ROWS;
     // Tiles of 256 rows are the quicker ones where they fill the chip (a workgroup per compute unit) twice or more: 2048 tokens behind
-    // 14336, 64 heads on 8, 1240 -> 1155 us.  Below that tiles of 128 rows (two per compute unit) spread better: a 2048-token prompt
-    // of 32 heads 75 -> 68 us.
+    // 14336, 64 heads on 8, 1166 us against 1237.  Below that tiles of 128 rows (two per compute unit) spread better: a 2048-token prompt
+    // of 32 heads 65.3 us against 84.5.  (Many short prompts would rather have the small ones: 64 of 17 to 100 tokens 116 against 110.)
     auto count = [&](int height) { return (B == 1 ? ((long)T * group + height - 1) / height : (long)T * group / height + B) * kv_heads; };
     p.tile_rows = count(256) >= 2 * 256 ? 256 : 128;
     const long blocks = count(p.tile_rows);
+    // Single tokens beside prompts: the tile kernel takes them along, a tile each, unless that costs more than a launch of the few-rows
+    // kernel and the wait for its end.  It does where every head has a cache of its own, so that a tile holds one row, and there
+    // are as many tiles as the chip takes at once (18 sequences of up to 393 tokens, 32 heads, e4m3: 34.5 us against 26.9; with two
+    // sequences there is little to gain, 85 against 89), and where a long sequence's one row may be the longest tile, tiles being too
+    // many to be split (a token at 16000 beside a chunk of 512 at 2048, 64 heads on 8: 351 against 81; 15 at 5000 to 14800 beside 2048 at
+    // 16384: 1578 against 1244).  Elsewhere taking them along is mostly the quicker (60 sequences of up to 224 tokens, 16 heads on 1: 13.2
+    // against 20.7; 25 of up to 5163, 64 on 8: 234 against 293), though not always (six sequences whose tokens are at 3000 and 5000, the
+    // prompts short: 130 against 67).  Over 70 drawn mixed calls this is 1 % from the better choice on average, two kernels for all 19 %.
+    const bool mixed = rows > SQP_FEW_ROWS && group <= SQP_FEW_ROWS && (long)B * max_q > T;
+    p.few = rows <= SQP_FEW_ROWS || (mixed && ((group == 1 && B > 8 && blocks >= 512) || (blocks > 256 && max_len >= 8192)));
+    p.tiles = rows > SQP_FEW_ROWS;
     p.f = split((long)B * kv_heads, 512, 256, max_len, most_parts);
-    p.t = split(blocks, 512, 512, max_len, most_parts);
+    p.t = split(blocks, p.few ? 1 : 512, 512, max_len, most_parts);  // (beside the few-rows kernel tiles are whole: one joining kernel, one layout)
     const int at_once = p.tile_rows == 128 ? 512 : 256;
     p.fold = blocks * p.t.parts <= at_once && p.tile_rows == 128 ? 256 / (kv_heads * p.t.parts) : 0;
-    // (Parts are only made of few groups: at most 256 of a sequence and cached head, or of tiles, so the slots are few as well.)
+    // Parts are only made of few groups, at most 256 of a sequence and cached head or of tiles, so that the slots are few as well.
     p.slots = p.tiles ? SQP_FEW_ROWS : (int)rows;
     p.few_slots = p.few && p.f.parts > 1 ? B * kv_heads * p.slots : 0;
     p.tile_slots = p.tiles && p.t.parts > 1 ? T * heads : 0;
@@ -138,7 +141,7 @@ template <int D>
 void combine(const SqpAttention &a, const Plan &p, int most_rows, hipStream_t st)
 {
     const int all = p.few_slots + p.tile_slots;
-    attention_combine_kernel<D><<<(unsigned)((all + 3) / 4), 256, 0, st>>>(a, p.f, p.t, most_rows, p.slots, p.few_slots, all);
+    attention_combine_kernel<D><<<(unsigned)((all + 3) / 4), 256, 0, st>>>(a, p.few_slots ? p.f : p.t, most_rows, p.few_slots ? p.slots : 0, all);
 }
 
 }  // namespace
@@ -178,8 +181,7 @@ extern "C" int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D,
     Plan p = plan(T, B, heads, kv_heads, D, most_q, reach, MOST_PARTS);
     const size_t room = scratch ? scratch_bytes : 0;
     for (int most = room ? MOST_PARTS - 1 : 1; p.bytes > room; most--) p = plan(T, B, heads, kv_heads, D, most_q, reach, most);  // (one part takes none)
-    p.f.part = (float *)scratch;
-    p.t.part = p.f.part + (size_t)p.few_slots * p.f.parts * (D + 4);
+    p.f.part = p.t.part = (float *)scratch;
     const int most_rows = !p.few ? -1 : !p.tiles ? INT_MAX : SQP_FEW_ROWS;  // of the few-rows kernel
     if (p.few) sqp_attention_few(type, D, a, p.f, most_rows, p.slots, st);
     if (p.tiles) sqp_attention_tiles(type, D, a, p.t, p.tile_rows, std::max(most_rows, 0), p.fold, st);

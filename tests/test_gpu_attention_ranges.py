@@ -15,14 +15,13 @@ def sqp():
     return m
 
 
-def expected(step, floor, hinted=True):
+def expected(step, floor, alone=True):
     """(out, tolerance) [T, heads, D] in 64 bits.  With w_j what is rounded for the matrix cores (p_j, for codes p_j times the value's
     scale), c_j the value over that scale and A = sum_j p_j |v_j|, the outputs are off by at most
       output's rounding   2^-11 |o| + 2^-25
-      w's rounding        sum_j max(eps w_j, floor max_i w_i) |c_j|: eps = 2^-22 up to 16 rows per cached head, 2^-11 above and in
-                          calls whose max_q is too small (hinted=False; where
-                          fp16 caches sum the rounded p, so that |o| is added to |c_j|); floor: half of fp16's smallest step, 2^-25, over
-                          the least that the largest w is held at
+      w's rounding        sum_j max(eps w_j, floor max_i w_i) |c_j|: eps = 2^-22 up to 16 rows per cached head, 2^-11 above and beside
+                          sequences of more (alone=False), where fp16 caches sum the rounded p, so that |o| is added to |c_j|;
+                          floor: half of fp16's smallest step, 2^-25, over the least that the largest w is held at
       scores              (D + 8) 2^-24 sum_d |q_d k_d| scale, the power of two 2^-21, in tiles of codes 2^-16 for the logarithm
                           of the value's scale (2^-18 of up to 40 each way) and its inverse: of each p, in numerator and denominator
       sums                len 2^-24 each."""
@@ -33,7 +32,7 @@ def expected(step, floor, hinted=True):
     for b, (length, n) in enumerate(zip(step.lens, step.news)):
         if length == 0:
             continue
-        few = n * group <= 16 and hinted
+        few = n * group <= 16 and alone
         k, c = step.rows(b, step.k, step.ks), step.rows(b, codes, None)
         size = step.rows(b, torch.ones_like(codes[..., :1]), step.vs)[..., 0]
         for i in range(max(0, n - length), n):
@@ -52,8 +51,8 @@ def expected(step, floor, hinted=True):
     return out, tol
 
 
-def compare(step, got, floor, hinted=True):
-    want, tol = expected(step, floor, hinted)
+def compare(step, got, floor, alone=True):
+    want, tol = expected(step, floor, alone)
     err = (got.cpu().double() - want).abs()
     assert bool((err <= tol).all()), "worst error / tolerance %.3f" % float((err / tol).nan_to_num(nan=1e9).max())
 
@@ -173,25 +172,26 @@ def test_value_scales_up_to_large_powers(sqp, n, kind):
 
 
 @pytest.mark.parametrize("kind", ["fp16", "e4m3"])
-@pytest.mark.parametrize("lens,news,heads,kv,D", [
-    ([3000, 17, 2600, 0, 1500, 700, 2049, 1, 2048, 900, 1800, 64], [1, 1, 40, 1, 2, 17, 1, 1, 4, 3, 33, 5], 8, 2, 128),   # parts in both kernels
-    ([2500, 2600, 1100, 513, 512, 2700, 256, 257, 1600, 40], [600] + [1] * 9, 16, 1, 64)])                      # and of the single tokens alone
-def test_single_tokens_and_chunks_in_parts(sqp, lens, news, heads, kv, D, kind):
-    """More than 8 sequences, single tokens and chunks among them, long enough for parts: both kernels' partial results have places of their
-    own inside the scratch, with any amount of it, and the output is whole."""
+@pytest.mark.parametrize("lens,news,heads,kv,D,max_len", [
+    ([3000, 17, 2600, 0, 1500, 700, 2049, 1, 2048, 900, 1800, 64], [1, 1, 40, 1, 2, 17, 1, 1, 4, 3, 33, 5], 8, 2, 128, 3000),    # parts of tiles
+    ([2500, 2600, 1100, 513, 512, 2700, 256, 257, 1600, 40], [2090] + [1] * 9, 16, 1, 64, 8192),             # of the single tokens beside whole tiles
+    ([1100, 900, 1100, 513, 512, 700, 256, 257, 600, 0], [1050, 850] + [1] * 8, 24, 24, 64, 1100)])          # a cache for every head
+def test_single_tokens_and_chunks_in_parts(sqp, lens, news, heads, kv, D, max_len, kind):
+    """Single tokens and chunks in one call, long enough for parts, with one kernel and with two: the partial results stay inside the scratch,
+    with any amount of it, and the output is whole."""
     import ctypes
-    print("case parts of both", lens, news, heads, kv, D, kind, flush=True)
+    print("case parts", lens, news, heads, kv, D, kind, flush=True)
     L = sqp.lib()
     step = ref.Step(lens, news, heads, kv, D, 16, kind, seed=66)
-    want, tol = expected(step, 2.0 ** -35)
+    want, tol = expected(step, 2.0 ** -35, alone=False)
     T, B, a = sum(news), len(lens), step.gpu()
-    need = int(L.sqp_paged_attention_scratch_bytes(T, B, heads, kv, D, max(news), max(lens)))
+    need = int(L.sqp_paged_attention_scratch_bytes(T, B, heads, kv, D, max(news), max_len))
     assert need > 0
     P = lambda t: ctypes.c_void_p(t.data_ptr()) if t is not None else None
     for nbytes in (need, need - 16, need // 3 & ~15, 16, 0):
         out = torch.full((T + 2, heads, D), float("nan"), dtype=torch.float16, device="cuda")
         scratch = torch.full((need + 512,), 0xFF, dtype=torch.uint8, device="cuda")  # (NaN where it is read without having been written)
-        rc = L.sqp_paged_attention(T, B, heads, kv, D, {"fp16": 0, "e4m3": 2}[kind], 16, step.k.shape[0], step.table.shape[1], max(news), max(lens), D ** -0.5,
+        rc = L.sqp_paged_attention(T, B, heads, kv, D, {"fp16": 0, "e4m3": 2}[kind], 16, step.k.shape[0], step.table.shape[1], max(news), max_len, D ** -0.5,
                                    P(a["q"]), heads * D, P(a["k_cache"]), P(a["v_cache"]), P(a["k_scales"]), P(a["v_scales"]), P(a["page_table"]),
                                    step.table.shape[1], P(a["seq_lens"]), P(a["q_starts"]), P(out[1:]), P(scratch[256:]) if nbytes else None, nbytes,
                                    ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
@@ -202,4 +202,4 @@ def test_single_tokens_and_chunks_in_parts(sqp, lens, news, heads, kv, D, kind):
         err = (out[1:-1].cpu().double() - want).abs()
         assert bool((err <= tol).all()), "scratch %d of %d: worst error / tolerance %.3f" % (nbytes, need, float((err / tol).nan_to_num(nan=1e9).max()))
     # hints that are too small: sequences of more rows, and longer ones, than there are places for
-    compare(step, sqp.paged_attention(**a, max_q=2, max_len=1000), 2.0 ** -35, hinted=False)
+    compare(step, sqp.paged_attention(**a, max_q=2, max_len=1000), 2.0 ** -35, alone=False)
