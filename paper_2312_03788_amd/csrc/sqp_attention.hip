@@ -121,7 +121,7 @@ Plan plan(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len, 
     // many to be split (a token at 16000 beside a chunk of 512 at 2048, 64 heads on 8: 351 against 81; 15 at 5000 to 14800 beside 2048 at
     // 16384: 1578 against 1244).  Elsewhere taking them along is mostly the quicker (60 sequences of up to 224 tokens, 16 heads on 1: 13.2
     // against 20.7; 25 of up to 5163, 64 on 8: 234 against 293), though not always (six sequences whose tokens are at 3000 and 5000, the
-    // prompts short: 130 against 67).  Over 70 drawn mixed calls this is 1 % from the better choice on average, two kernels for all 19 %.
+    // prompts short: 130 against 67).  Over 70 drawn mixed calls this is 1 % from the better choice on average, two kernels for all 21 %.
     const bool mixed = rows > SQP_FEW_ROWS && group <= SQP_FEW_ROWS && (long)B * max_q > T;
     p.few = rows <= SQP_FEW_ROWS || (mixed && ((group == 1 && B > 8 && blocks >= 512) || (blocks > 256 && max_len >= 8192)));
     p.tiles = rows > SQP_FEW_ROWS;

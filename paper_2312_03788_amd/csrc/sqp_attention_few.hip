@@ -14,12 +14,13 @@
 // at up to 2500 tokens take 286 us instead of 147.
 //
 // The matrix cores wait for memory here, so p goes through them twice: rounded to fp16, and what that leaves, in fp16 again (2^-22
-// of p then, or 2^-35 of the row's largest where that is more).  The output's rounding is the only one left: the error of 8192-token outputs is 2.1e-4 of them instead of 3.0e-4, in
-// the same time (45.0 and 45.1 us with the 16 sequences below, 147.0 and 147.1 with the 32).
+// of p then, or 2^-35 of the row's largest where that is more).  The output's rounding is the only one left: the error of the 32
+// sequences' outputs below is 2.1e-4 of them instead of 2.6e-4, in the same time (149.2 us and 149.4); over codes it costs up to 3 % (16
+// sequences 39.0 us instead of 38.3, called again and again on the same cache).
 //
-// Measured, kernel alone: those 800 MB in 146 us (5.5 TB/s; a streaming read alone reaches 5.9 on this chip); one sequence of 32000
-// tokens, 40 heads, int8, 338 MB in 59 us (5.7 TB/s); 16 at up to 8192, 8 cached heads, e4m3, 166 MB in 34 to 37 us from box to box (4.9 TB/s,
-// parts of unequal length).  32 heads over 129 tokens: 6.2 us, the chain length, page, K, V.
+// Measured, kernel alone: those 800 MB in 149 us (5.4 TB/s; a streaming read alone reaches 5.9 on this chip); one sequence of 32000
+// tokens, 40 heads, int8, 338 MB in 61 us (5.5 TB/s); 16 at up to 8192, 8 cached heads, e4m3, 166 MB in 36 us (4.6 TB/s, parts of unequal
+// length).  32 heads over 129 tokens: 6.1 us, the chain length, page, K, V.
 #include "sqp_attention.h"
 
 namespace {

@@ -19,12 +19,12 @@
 // tile ahead of their storing; with three tiles of V (8 waves) that is one barrier per 64 tokens, with two (4 waves, two
 // workgroups per compute unit) it is two.
 //
-// Measured: 2048 tokens behind 14336, 64 heads on 8, e4m3: 1070 to 1160 us from box to box, 890 to 960 TFLOP/s, where a large dense
+// Measured: 2048 tokens behind 14336, 64 heads on 8, e4m3: 1080 to 1170 us from box to box, 880 to 950 TFLOP/s, where a large dense
 // fp16 product of the library reaches 1134 and a loop of matrix instructions alone 1572: all of them run at the clock that the
 // power limit leaves (1.8 of 2.4 GHz here).  A tile of 64 tokens takes a compute unit 2.2 to 2.35 us; without staging, maxima,
-// exponentials and barriers it still takes 1.8 to 2.0.  A 2048-token prompt of 32 heads: 57.5 us; its longest tile goes through
+// exponentials and barriers it still takes 1.8 to 2.0.  A 2048-token prompt of 32 heads: 59.4 us; its longest tile goes through
 // 32 steps of 64 tokens alone on its compute unit at 1.4 to 1.9 us each, in which latencies show that a second wave would hide.
-// Dropped: 64 rows per wave with one wave per SIMD (half the reads of shared memory, but nothing hides what the order of
+// Dropped (figures of the kernel as it was then): 64 rows per wave with one wave per SIMD (half the reads of shared memory, but nothing hides what the order of
 // instructions does not: 1288 us where 128-row tiles took 1240); stores spread over a step (their loads have less time: the
 // prompt 68.6 -> 74.6 us); K in shared memory with its scale multiplied in (a rounding more in the scores); p cut to 11 bits before
 // the sum takes it too, so that its error leaves rows that a few tokens rule (worst of 70 cases 1.37 times the output's rounding
