@@ -239,6 +239,32 @@ int sqp_alpha_search_scratch(int T, int N, int K, int group, int n_alpha, const 
 #define SQP_FP16 0
 #define SQP_INT8 1
 #define SQP_E4M3 2
+/* Microscaled numbers: blocks of 32 values along a row.  SQP_E2M1: 4 bits, 2 of exponent and 1 of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives, two to a byte, the first in the low half; or elements SQP_E4M3.  A block has one scale in a byte b: its values are
+ * code * 2^(b - 127).  The scale of a block is the least power of two with which its largest magnitude rounds to a value of the type,
+ * so that no value is cut off; code = round-to-nearest-even(value / scale).  A block whose largest magnitude is below 2^-100 is
+ * stored as zeros with b = 0, one with an infinity or NaN as zeros with b = 255, which stands for NaN: all of it reads back as NaN.
+ * Negative values that round to zero keep their sign. */
+#define SQP_E2M1 4
+
+/* Rows into blocks of `type` (SQP_E2M1 or SQP_E4M3) and back.  x [R][K] fp16, K % 32 == 0; codes [R][K/2] bytes (e2m1) or [R][K];
+ * scales [R][K/32] bytes.  Back: x = fp16(code * scale), one rounding (values beyond fp16's largest become infinite). */
+int sqp_mx_quantize(int R, int K, int type, const void *x, void *codes, uint8_t *scales, void *stream);
+int sqp_mx_dequantize(int R, int K, int type, const void *codes, const uint8_t *scales, void *x, void *stream);
+
+/* A weight w [K][N] fp16 (the orientation of Eq. 2, already smoothed) into e2m1 blocks along K: one row per output column, codes
+ * [N][K/2], scales [N][K/32], which is what sqp_mx_quantize gives for w transposed.  K % 32 == 0, N % 8 == 0. */
+int sqp_mx_quantize_weight(int N, int K, const void *w, void *codes, uint8_t *scales, void *stream);
+
+/* The linear layer on blocks: y[m][n] = fp16( sum_k x[m][k] w[n][k] ), the products of the codes multiplied by both blocks' scales on
+ * the matrix cores and summed in fp32, one rounding at the end.  x: M rows of x_type (SQP_E2M1 or SQP_E4M3) with their scales, w: N rows of e2m1 with
+ * theirs.  M, N, K > 0, N % 8 == 0, K % 32 == 0.  silu_mul != 0: the columns alternate (gate j, up j) (sqp_interleave_gate_up), N % 16 == 0, and
+ * y [M][N/2] = fp16(SiLU(g) u) of the fp32 sums.  A block that is NaN makes NaN of its row (x) or column (w).  Deterministic.
+ * scratch: of this call alone until its work has run, sqp_mx_gemm_scratch_bytes() for the preferred plan; smaller or NULL:
+ * a plan that fits.  No other workspace: calls may overlap with anything. */
+size_t sqp_mx_gemm_scratch_bytes(int M, int N, int K, int x_type);
+int sqp_mx_gemm(int M, int N, int K, int x_type, int silu_mul, const void *x, const uint8_t *x_scales, const void *w, const uint8_t *w_scales,
+                void *y, void *scratch, size_t scratch_bytes, void *stream);
 
 /* The residual's addition and the RMS norm behind it: sum = fp16(x + residual), y = sqp_rmsnorm(sum) (fp32 arithmetic, one
  * rounding at the end).  x, residual, sum, y [M][H] fp16, gamma [H] fp16, H % 8 == 0, 0 <= eps < 1.  sum may be x or residual
@@ -249,9 +275,15 @@ int sqp_add_rmsnorm(int M, int H, const void *x, const void *residual, const voi
 int sqp_add_rmsnorm_quant(int M, int H, int type, const void *x, const void *residual, const void *gamma, float eps, void *codes,
                           float *scales, void *sum, void *stream);
 
+/* The same with y in blocks of `type` (SQP_E2M1 or SQP_E4M3), H % 32 == 0: codes [M][H/2] or [M][H], scales [M][H/32] bytes.  The codes are
+ * those of y in 64-bit arithmetic, rounded once. */
+int sqp_add_rmsnorm_mx(int M, int H, int type, const void *x, const void *residual, const void *gamma, float eps, void *codes,
+                       uint8_t *scales, void *sum, void *stream);
+
 /* Paged cache of keys and values, D = 64 or 128 values per token and head, `page` tokens per page (a power of two from 16 to 65536):
  *   k_cache, v_cache    [pages][kv_heads][page][D] of `type`; pages * page < 2^31, the tensors may have more elements than that
  *   k_scales, v_scales  [pages][kv_heads][page] fp32 (8-bit types; NULL for SQP_FP16)
+ * or blocks of SQP_E2M1: k_cache, v_cache [pages][kv_heads][page][D/2] bytes, k_scales, v_scales [pages][kv_heads][page][D/32] bytes.
  * A slot is a token's place: page number * page + place in the page.  Index arrays (slots, positions, page tables, lengths,
  * starts) are int32 and need 4-byte alignment only.
  *
@@ -264,11 +296,11 @@ int sqp_add_rmsnorm_quant(int M, int H, int type, const void *x, const void *res
  * T == 0 enqueues nothing. */
 int sqp_kv_cache_write(int T, int heads, int kv_heads, int D, int type, int page, int pages, const void *q, long q_stride, const void *k,
                        long k_stride, const void *v, long v_stride, const int *slots, const float *cos_sin, const int *positions,
-                       int n_positions, void *k_cache, void *v_cache, float *k_scales, float *v_scales, void *q_out, void *stream);
+                       int n_positions, void *k_cache, void *v_cache, void *k_scales, void *v_scales, void *q_out, void *stream);
 
 /* Reads T slots back: k, v [T][kv_heads][D] fp16 = fp16(code * scale); zeros for a slot outside the cache. */
 int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages, const int *slots, const void *k_cache, const void *v_cache,
-                      const float *k_scales, const float *v_scales, void *k, void *v, void *stream);
+                      const void *k_scales, const void *v_scales, void *k, void *v, void *stream);
 
 /* Attention of the newest tokens of B sequences over the paged cache, which holds these tokens' keys and values already:
  *   out[t][h] = sum_j p_j v_j,  p = softmax_j (scale q[t][h] . k_j),  h reading the cached head h / (heads / kv_heads)
@@ -292,8 +324,8 @@ int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages,
  * starts past T are taken as the nearest that is inside.  Deterministic.  B <= 65535. */
 size_t sqp_paged_attention_scratch_bytes(int T, int B, int heads, int kv_heads, int D, int max_q, int max_len);
 int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D, int type, int page, int pages, int table_width, int max_q, int max_len,
-                        float scale, const void *q, long q_stride, const void *k_cache, const void *v_cache, const float *k_scales,
-                        const float *v_scales, const int *page_table, long table_stride, const int *seq_lens, const int *q_starts, void *out,
+                        float scale, const void *q, long q_stride, const void *k_cache, const void *v_cache, const void *k_scales,
+                        const void *v_scales, const int *page_table, long table_stride, const int *seq_lens, const int *q_starts, void *out,
                         void *scratch, size_t scratch_bytes, void *stream);
 
 #pragma GCC visibility pop

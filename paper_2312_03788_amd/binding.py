@@ -18,7 +18,8 @@ EXPORTS = ["sqp_status_string", "sqp_smooth_scales", "sqp_smooth_apply_x", "sqp_
            "sqp_quantize_pack", "sqp_dequantize", "sqp_w4a16_gemm", "sqp_quant_loss", "sqp_transpose_nk",
            "sqp_w4a16_gemm_silu_mul", "sqp_rmsnorm", "sqp_scale_columns", "sqp_interleave_gate_up",
            "sqp_set_workspace", "sqp_alpha_search", "sqp_w4a16_gemm_static", "sqp_w4a16_gemm_scratch", "sqp_alpha_search_scratch",
-           "sqp_add_rmsnorm", "sqp_add_rmsnorm_quant", "sqp_kv_cache_write", "sqp_kv_cache_read", "sqp_paged_attention"]
+           "sqp_add_rmsnorm", "sqp_add_rmsnorm_quant", "sqp_kv_cache_write", "sqp_kv_cache_read", "sqp_paged_attention",
+           "sqp_mx_quantize", "sqp_mx_dequantize", "sqp_mx_quantize_weight", "sqp_mx_gemm", "sqp_add_rmsnorm_mx"]
 
 
 class SqpError(RuntimeError):
@@ -75,6 +76,13 @@ def lib():
         L.sqp_paged_attention.argtypes = [i] * 11 + [f, vp, ll, vp, vp, vp, vp, vp, ll, vp, vp, vp, vp, sz, vp]
         L.sqp_paged_attention_scratch_bytes.argtypes = [i] * 7
         L.sqp_paged_attention_scratch_bytes.restype = sz
+        L.sqp_mx_quantize.argtypes = [i, i, i, vp, vp, vp, vp]
+        L.sqp_mx_dequantize.argtypes = [i, i, i, vp, vp, vp, vp]
+        L.sqp_mx_quantize_weight.argtypes = [i, i, vp, vp, vp, vp]
+        L.sqp_mx_gemm.argtypes = [i] * 5 + [vp] * 6 + [sz, vp]
+        L.sqp_mx_gemm_scratch_bytes.argtypes = [i] * 4
+        L.sqp_mx_gemm_scratch_bytes.restype = sz
+        L.sqp_add_rmsnorm_mx.argtypes = [i, i, i, vp, vp, vp, f, vp, vp, vp, vp]
         for name in EXPORTS[1:]:
             getattr(L, name).restype = ctypes.c_int
         L.sqp_quant_loss_scratch_doubles.restype = ctypes.c_long
@@ -90,6 +98,8 @@ def lib():
         fast.bind_layer(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.sqp_add_rmsnorm, L.sqp_add_rmsnorm_quant, L.sqp_kv_cache_write, L.sqp_kv_cache_read, L.sqp_paged_attention,
             L.sqp_paged_attention_scratch_bytes)])
+        fast.bind_mx(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.sqp_mx_quantize, L.sqp_mx_dequantize, L.sqp_mx_quantize_weight, L.sqp_mx_gemm, L.sqp_mx_gemm_scratch_bytes, L.sqp_add_rmsnorm_mx)])
         _fast = fast
         _lib = L
     return _lib
@@ -449,6 +459,7 @@ def alpha_search(x_cal, w, group=128, alphas=None):
 # ---------------------------------------------------------------- between the linears: residual and norm, cache, attention
 
 _TYPES = {torch.float16: 0, torch.int8: 1, torch.float8_e4m3fn: 2}  # SQP_FP16, SQP_INT8, SQP_E4M3
+_CACHE_TYPES = {**_TYPES, torch.uint8: 4}  # SQP_E2M1: two codes to a byte
 
 
 def add_rmsnorm(x, residual, gamma, eps, out=None, sum_out=None):
@@ -519,12 +530,19 @@ def _step(t):
 
 def _cache(k_cache, v_cache, k_scales, v_scales):
     """Arguments of a cache: (pages, kv_heads, page, D, type) and its four pointers."""
-    if k_cache.dim() != 4 or k_cache.dtype not in _TYPES:
-        raise SqpError("k_cache must be [pages, kv_heads, page, D] of torch.float16, torch.int8 or torch.float8_e4m3fn")
+    if k_cache.dim() != 4 or k_cache.dtype not in _CACHE_TYPES:
+        raise SqpError("k_cache must be [pages, kv_heads, page, D] of torch.float16, torch.int8 or torch.float8_e4m3fn, or [pages, kv_heads, page, D/2] of torch.uint8")
     _shaped(v_cache, k_cache.shape, "v_cache")
     ptrs = [_dev(k_cache, k_cache.dtype, "k_cache"), _dev(v_cache, k_cache.dtype, "v_cache"), None, None]
-    kind = _TYPES[k_cache.dtype]
-    if kind:
+    kind, D = _CACHE_TYPES[k_cache.dtype], k_cache.shape[3]
+    if kind == 4:
+        D = 2 * D
+        for at, (s, name) in enumerate(((k_scales, "k_scales"), (v_scales, "v_scales"))):
+            if s is None:
+                raise SqpError("a cache of e2m1 blocks needs %s" % name)
+            _shaped(s, tuple(k_cache.shape[:3]) + (D // 32,), name)
+            ptrs[2 + at] = _dev(s, torch.uint8, name)
+    elif kind:
         for at, (s, name) in enumerate(((k_scales, "k_scales"), (v_scales, "v_scales"))):
             if s is None:
                 raise SqpError("an 8-bit cache needs %s" % name)
@@ -532,12 +550,13 @@ def _cache(k_cache, v_cache, k_scales, v_scales):
             ptrs[2 + at] = _dev(s, torch.float32, name)
     elif k_scales is not None or v_scales is not None:
         raise SqpError("an fp16 cache has no scales")
-    return tuple(k_cache.shape) + (kind,), ptrs
+    return tuple(k_cache.shape[:3]) + (D, kind), ptrs
 
 
 def kv_cache_write(k, v, slots, k_cache, v_cache, k_scales=None, v_scales=None, q=None, cos_sin=None, positions=None, out=None):
     """Keys and values [T, kv_heads, D] of T tokens into their slots (page * tokens per page + place; int32 [T], outside the
-    cache: not written) of the cache [pages, kv_heads, page, D] (fp16, or int8 / e4m3 with scales [pages, kv_heads, page]).
+    cache: not written) of the cache [pages, kv_heads, page, D] (fp16, or int8 / e4m3 with scales [pages, kv_heads, page]; or e2m1 blocks, two codes to a byte:
+    uint8 [pages, kv_heads, page, D/2] with scales uint8 [pages, kv_heads, page, D/32]).
     With cos_sin [positions, D] fp32 and positions int32 [T], keys and q are rotated; returns the queries [T, heads, D], or None
     without q.  q, k and v may be views of a merged projection."""
     if _fast is not None and isinstance(k, _Tensor) and k.is_cuda:
@@ -641,3 +660,152 @@ def paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts=None, k_
                                          qp, _step(q), *cache, table, page_table.stride(0) if B > 1 else width, lens, starts, op,
                                          ctypes.c_void_p(scratch.data_ptr()) if scratch is not None else None, nbytes, _stream()), "sqp_paged_attention")
     return o
+
+
+# ---------------------------------------------------------------- microscaled numbers: blocks of 32 with a power-of-two scale
+
+_MX_TYPES = {torch.uint8: 4, torch.float8_e4m3fn: 2}  # SQP_E2M1 (two codes to a byte), SQP_E4M3
+
+
+def _mx_kind(dtype):
+    if dtype not in _MX_TYPES:
+        raise SqpError("dtype must be torch.uint8 (e2m1, two codes to a byte) or torch.float8_e4m3fn")
+    return _MX_TYPES[dtype]
+
+
+def _mx_width(K, kind):
+    return K // 2 if kind == 4 else K
+
+
+def _mx_out(out, R, K, kind, dtype, device):
+    """(codes, scales) of R rows of K values, given or new."""
+    if K % 32:
+        raise SqpError("rows must be whole blocks of 32 values")
+    codes, scales = out if out is not None else (torch.empty((R, _mx_width(K, kind)), dtype=dtype, device=device),
+                                                 torch.empty((R, K // 32), dtype=torch.uint8, device=device))
+    _shaped(codes, (R, _mx_width(K, kind)), "codes")
+    _shaped(scales, (R, K // 32), "scales")
+    return codes, scales
+
+
+def _mx_rows(codes, scales, name):
+    """(rows, values per row, type) of codes [R, K/2] uint8 or [R, K] e4m3 with scales [R, K/32]."""
+    if codes.dim() != 2 or codes.dtype not in _MX_TYPES:
+        raise SqpError("%s must be [rows, K/2] of torch.uint8 or [rows, K] of torch.float8_e4m3fn" % name)
+    kind = _MX_TYPES[codes.dtype]
+    R, K = codes.shape[0], codes.shape[1] * (2 if kind == 4 else 1)
+    if K % 32:
+        raise SqpError("%s must hold whole blocks of 32 values" % name)
+    _shaped(scales, (R, K // 32), "%s's scales" % name)
+    return R, K, kind
+
+
+def mx_quantize(x, dtype=torch.uint8, out=None):
+    """(codes, scales): rows x [R, K] fp16 in blocks of 32 values with one power-of-two scale each (K a multiple of 32): codes
+    [R, K/2] uint8 (e2m1, two to a byte) or [R, K] torch.float8_e4m3fn, scales [R, K/32] uint8 (the exponent plus 127)."""
+    if out is None and _fast is not None and isinstance(x, _Tensor) and x.is_cuda:
+        dev = _current_device()
+        o = _fast.mx_quantize(_MX_TYPES.get(dtype, 0), x, dev, _raw_stream(dev))
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_mx_quantize")
+    kind = _mx_kind(dtype)
+    R, K = x.shape
+    codes, scales = _mx_out(out, R, K, kind, dtype, x.device)
+    _check(lib().sqp_mx_quantize(R, K, kind, _dev(x, torch.float16, "x"), _dev(codes, dtype, "codes"), _dev(scales, torch.uint8, "scales"), _stream()),
+           "sqp_mx_quantize")
+    return codes, scales
+
+
+def mx_quantize_weight(w, out=None):
+    """(codes [N, K/2] uint8, scales [N, K/32] uint8): a weight w [K, N] fp16 in e2m1 blocks along K, a row per output column."""
+    if out is None and _fast is not None and isinstance(w, _Tensor) and w.is_cuda:
+        dev = _current_device()
+        o = _fast.mx_quantize_weight(w, dev, _raw_stream(dev))
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_mx_quantize_weight")
+    K, N = w.shape
+    codes, scales = _mx_out(out, N, K, 4, torch.uint8, w.device)
+    _check(lib().sqp_mx_quantize_weight(N, K, _dev(w, torch.float16, "w"), _dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), _stream()),
+           "sqp_mx_quantize_weight")
+    return codes, scales
+
+
+def mx_dequantize(codes, scales, out=None):
+    """What codes and scales stand for, fp16 [R, K] (a weight's codes: its columns as rows)."""
+    if out is None and _fast is not None and isinstance(codes, _Tensor) and codes.is_cuda:
+        dev = _current_device()
+        o = _fast.mx_dequantize(codes, scales, dev, _raw_stream(dev))
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_mx_dequantize")
+    R, K, kind = _mx_rows(codes, scales, "codes")
+    x = out if out is not None else torch.empty((R, K), dtype=torch.float16, device=codes.device)
+    _shaped(x, (R, K), "out")
+    _check(lib().sqp_mx_dequantize(R, K, kind, _dev(codes, codes.dtype, "codes"), _dev(scales, torch.uint8, "scales"), _dev(x, torch.float16, "out"), _stream()),
+           "sqp_mx_dequantize")
+    return x
+
+
+def _mx_gemm(silu, x, x_scales, w, w_scales, out):
+    """The product's general path."""
+    M, K, kind = _mx_rows(x, x_scales, "x")
+    N, K2, w_kind = _mx_rows(w, w_scales, "w")
+    if w_kind != 4:
+        raise SqpError("w must be e2m1 (torch.uint8)")
+    if K != K2:
+        raise SqpError("x and w disagree on K")
+    y = out if out is not None else torch.empty((M, N // 2 if silu else N), dtype=torch.float16, device=x.device)
+    _shaped(y, (M, N // 2 if silu else N), "out")
+    args = [M, N, K, kind, silu, _dev(x, x.dtype, "x"), _dev(x_scales, torch.uint8, "x_scales"), _dev(w, torch.uint8, "w"), _dev(w_scales, torch.uint8, "w_scales"),
+            _dev(y, torch.float16, "out")]
+    scratch, nbytes = None, 0
+    if not (out is not None and torch.cuda.is_current_stream_capturing()):
+        nbytes = int(lib().sqp_mx_gemm_scratch_bytes(M, N, K, kind))
+        if nbytes:
+            try:
+                scratch = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+            except torch.cuda.OutOfMemoryError:
+                nbytes = 0
+    _check(lib().sqp_mx_gemm(*args, ctypes.c_void_p(scratch.data_ptr()) if scratch is not None else None, nbytes, _stream()), "sqp_mx_gemm")
+    return y
+
+
+def mx_gemm(x, x_scales, w, w_scales, out=None):
+    """y [M, N] fp16 = x w^T on microscaled operands: x as mx_quantize gives it (either type), w as mx_quantize_weight does.
+    Under graph capture a call with `out` allocates nothing, so that K is not split over workgroups."""
+    if _fast is not None and isinstance(x, _Tensor) and x.is_cuda:
+        dev = _current_device()
+        o = _fast.mx_gemm(0, x, x_scales, w, w_scales, out, dev, _raw_stream(dev))
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_mx_gemm")
+    return _mx_gemm(0, x, x_scales, w, w_scales, out)
+
+
+def mx_gemm_silu_mul(x, x_scales, w, w_scales, out=None):
+    """mx_gemm of a merged, interleaved gate/up weight with SiLU(gate) * up fused: y [M, N/2] fp16."""
+    if _fast is not None and isinstance(x, _Tensor) and x.is_cuda:
+        dev = _current_device()
+        o = _fast.mx_gemm(1, x, x_scales, w, w_scales, out, dev, _raw_stream(dev))
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_mx_gemm")
+    return _mx_gemm(1, x, x_scales, w, w_scales, out)
+
+
+def add_rmsnorm_mx(x, residual, gamma, eps, dtype=torch.uint8, out=None, sum_out=None):
+    """(codes, scales, r): add_rmsnorm with y in blocks as mx_quantize gives them, but from y before any rounding to fp16 (H a
+    multiple of 32).  out: (codes, scales)."""
+    if out is None and _fast is not None and isinstance(x, _Tensor) and x.is_cuda:
+        dev = _current_device()
+        o = _fast.add_rmsnorm_mx(_MX_TYPES.get(dtype, 0), x, residual, gamma, eps, sum_out, dev, _raw_stream(dev))
+        if o is not None:
+            return o if type(o) is not int else _ended(o, "sqp_add_rmsnorm_mx")
+    kind = _mx_kind(dtype)
+    M, H = x.shape
+    _shaped(residual, (M, H), "residual")
+    _shaped(gamma, (H,), "gamma")
+    codes, scales = _mx_out(out, M, H, kind, dtype, x.device)
+    r = sum_out if sum_out is not None else torch.empty_like(x)
+    _shaped(r, (M, H), "sum_out")
+    _check(lib().sqp_add_rmsnorm_mx(M, H, kind, _dev(x, torch.float16, "x"), _dev(residual, torch.float16, "residual"), _dev(gamma, torch.float16, "gamma"),
+                                    float(eps), _dev(codes, dtype, "codes"), _dev(scales, torch.uint8, "scales"), _dev(r, torch.float16, "sum_out"), _stream()),
+           "sqp_add_rmsnorm_mx")
+    return codes, scales, r

@@ -5,15 +5,14 @@
 // t being one of the n newest tokens of a sequence of `len` cached ones (the new ones among them): token i of the n sees
 // j <= len - n + i.  Query head h reads the cached head h / (heads / kv_heads).
 #pragma once
-#include "sqp_rows.h"
+#include "sqp_mx.h"
 
 struct SqpAttention {
     int T, B, heads, kv_heads, group;  // group: query heads per cached head
     int page_shift, pages, table_width;
     long q_stride, table_stride;
     const h16 *q;
-    const void *k, *v;
-    const float *k_scales, *v_scales;
+    const void *k, *v, *k_scales, *v_scales;
     const int *table, *lens, *starts;  // starts == nullptr: one new token per sequence
     h16 *out;
     float scale2;  // scale log2(e): the softmax is taken in powers of two
@@ -71,6 +70,32 @@ __device__ __forceinline__ float sqp_known_scale(float scale)
 }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <int TYPE, int D> constexpr int SQP_ROW_BYTES = D * (TYPE == SQP_FP16 ? 4 : TYPE == SQP_E2M1 ? 1 : 2) / 2;  // of a cached key or value
+
+// e2m1 blocks become fp16 values on their way to the matrix cores, which then work as over an fp16 cache: keys half their size (a
+// rotated key of fp16 parts reaches 92640, its block 6 x 2^14; the scores' factor makes up for it), values as they are.  What is below
+// fp16's smallest step is rounded as in an fp16 cache.  A block too large for fp16, which only values of 57344 on make, or keys that no
+// fp16 pair does, becomes NaN, and the rows that see it are computed one by one.
+__device__ __forceinline__ float sqp_key_scale(uint32_t byte) { return __builtin_bit_cast(float, byte > 141u ? 0x7f800000u : (max(byte, 1u) - 1u) << 23); }
+__device__ __forceinline__ float sqp_value_scale(uint32_t byte) { return __builtin_bit_cast(float, byte > 140u ? 0x7f800000u : byte << 23); }
+
+// Eight codes of a word in fp16 (a scale that is not finite makes NaN of them).
+__device__ __forceinline__ h16x8 sqp_e2m1_halves8(uint32_t w, float scale)
+{
+    const h16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1);
+    const h16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
+    return h16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+// Two codes of byte `at` (a constant once loops are unrolled).
+__device__ __forceinline__ uint32_t sqp_e2m1_halves2(uint32_t w, float scale, int at)
+{
+    return __builtin_bit_cast(uint32_t, at == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)
+                                        : at == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)
+                                        : at == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)
+                                                  : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3));
+}
 
 // BYTES bytes as words.
 template <int BYTES>
@@ -227,6 +252,23 @@ __device__ __forceinline__ void sqp_attend_row(const SqpAttention &a, const h16 
                 for (int e = 0; e < 8; e++) s += x[e] * (float)q[8 * i + e];
             }
             s *= a.scale2;
+        } else if constexpr (TYPE == SQP_E2M1) {
+            const uint4 *kp = (const uint4 *)((const uint8_t *)a.k + row * (D / 2));
+            const uint8_t *kb = (const uint8_t *)a.k_scales + row * (D / 32);
+#pragma unroll 1
+            for (int i = 0; i < D / 32; i++) {
+                const uint4 w = kp[i];
+                const uint32_t c[4] = {w.x, w.y, w.z, w.w};
+                const float step = __builtin_bit_cast(float, (uint32_t)kb[i] << 23);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    float x[8];
+                    sqp_mx_e2m1_values8(c[e], step, x);
+#pragma unroll
+                    for (int j = 0; j < 8; j++) s += x[j] * (float)q[32 * i + 8 * e + j];
+                }
+            }
+            s *= 0.5f * a.scale2;  // (scale2 is that of keys of half their size)
         } else {
             const uint4 *kp = (const uint4 *)((const uint8_t *)a.k + row * D);
 #pragma unroll 1
@@ -241,8 +283,8 @@ __device__ __forceinline__ void sqp_attend_row(const SqpAttention &a, const h16 
                     s += (float)x.x * (float)qe[0] + (float)x.y * (float)qe[1] + (float)y.x * (float)qe[2] + (float)y.y * (float)qe[3];
                 }
             }
-            s *= a.k_scales[row] * a.scale2;
-            vs = a.v_scales[row];
+            s *= ((const float *)a.k_scales)[row] * a.scale2;
+            vs = ((const float *)a.v_scales)[row];
         }
         if (base + lane >= hi) s = -INFINITY;
         float top = s;
@@ -266,6 +308,13 @@ __device__ __forceinline__ void sqp_attend_row(const SqpAttention &a, const h16 
                 const h16 *vp = (const h16 *)a.v + vrow * D + PER * lane;
 #pragma unroll
                 for (int e = 0; e < PER; e++) o[e] += pj * (float)vp[e];
+            } else if constexpr (TYPE == SQP_E2M1) {
+                const uint32_t w = ((const uint8_t *)a.v)[vrow * (D / 2) + PER * lane / 2] >> (PER == 2 ? 0 : 4 * (lane & 1));
+                const float step = __builtin_bit_cast(float, (uint32_t)((const uint8_t *)a.v_scales)[vrow * (D / 32) + PER * lane / 32] << 23);
+                float x[8];
+                sqp_mx_e2m1_values8(w, step, x);
+#pragma unroll
+                for (int e = 0; e < PER; e++) o[e] += pj * x[e];
             } else {
                 const uint8_t *vp = (const uint8_t *)a.v + vrow * D + PER * lane;
                 const uint32_t w = PER == 2 ? *(const uint16_t *)vp : *vp;

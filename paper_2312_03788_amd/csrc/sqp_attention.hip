@@ -5,7 +5,7 @@
 
 #include "sqp_attention.h"
 
-int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const void *k_cache, const void *v_cache, const float *k_scales, const float *v_scales);
+int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const void *k_cache, const void *v_cache, const void *k_scales, const void *v_scales);
 
 namespace {
 
@@ -153,8 +153,8 @@ extern "C" size_t sqp_paged_attention_scratch_bytes(int T, int B, int heads, int
 }
 
 extern "C" int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D, int type, int page, int pages, int table_width, int max_q, int max_len,
-                                   float scale, const void *q, long q_stride, const void *k_cache, const void *v_cache, const float *k_scales,
-                                   const float *v_scales, const int *page_table, long table_stride, const int *seq_lens, const int *q_starts, void *out,
+                                   float scale, const void *q, long q_stride, const void *k_cache, const void *v_cache, const void *k_scales,
+                                   const void *v_scales, const int *page_table, long table_stride, const int *seq_lens, const int *q_starts, void *out,
                                    void *scratch, size_t scratch_bytes, void *stream)
 {
     const int rc = sqp_check_cache(kv_heads, D, type, page, pages, k_cache, v_cache, k_scales, v_scales);
@@ -175,7 +175,7 @@ extern "C" int sqp_paged_attention(int T, int B, int heads, int kv_heads, int D,
     a.q_stride = q_stride; a.table_stride = table_stride;
     a.q = (const h16 *)q; a.k = k_cache; a.v = v_cache; a.k_scales = k_scales; a.v_scales = v_scales;
     a.table = page_table; a.lens = seq_lens; a.starts = q_starts; a.out = (h16 *)out;
-    a.scale2 = scale * 1.44269504088896340736f;
+    a.scale2 = scale * (type == SQP_E2M1 ? 2.0f : 1.0f) * 1.44269504088896340736f;  // (blocks' keys are taken at half their size)
     hipStream_t st = (hipStream_t)stream;
     const int reach = max_len > 0 ? max_len : table_width * page, most_q = q_starts ? max_q : 1;
     Plan p = plan(T, B, heads, kv_heads, D, most_q, reach, MOST_PARTS);

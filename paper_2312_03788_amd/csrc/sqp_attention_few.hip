@@ -28,9 +28,12 @@ namespace {
 template <int TYPE, int D>
 __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttention a, SqpParts parts, int most_rows, int slots)
 {
-    constexpr int BYTES = SqpCode<TYPE>::BYTES;
-    constexpr int KL = D * BYTES / 64;       // 16-byte loads per lane and 16 keys
-    constexpr int VW = D * BYTES / 64;       // words per lane and token of V
+    constexpr bool BLOCKS = TYPE == SQP_E2M1, CODES = TYPE != SQP_FP16 && !BLOCKS;  // (codes with a scale per token)
+    constexpr int BYTES = TYPE == SQP_FP16 ? 2 : 1, ROW = SQP_ROW_BYTES<TYPE, D>;
+    constexpr int KB = ROW / 4 < 16 ? ROW / 4 : 16;  // bytes of a lane's load of a key: the four lanes have the whole row (codes: 64 bytes at a time)
+    constexpr int KL = ROW / (4 * KB);       // loads per lane and 16 keys
+    constexpr int VB = ROW / 16, VW = (VB + 3) / 4;  // bytes and words per lane and token of V
+    constexpr int SB = D / 32;               // bytes of scales per token (blocks)
     constexpr int DPL = D / 16;              // dimensions per lane of V
     constexpr int NB = TYPE == SQP_FP16 ? 2 : 4;  // blocks of 16 tokens per step: codes are half as long, so twice as many keep
                                                   // the same number of bytes on their way
@@ -62,7 +65,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
         {
             const h16 *q = a.q + (size_t)(s.first + token) * a.q_stride + head * D;
 #pragma unroll
-            for (int i = 0; i < D / 32; i++) qf[i] = *(const h16x8 *)(q + (BYTES == 2 ? 32 * i + 8 * g : 64 * (i >> 1) + 16 * g + 8 * (i & 1)));
+            for (int i = 0; i < D / 32; i++) qf[i] = *(const h16x8 *)(q + (BLOCKS ? D / 4 * g + 8 * i : BYTES == 2 ? 32 * i + 8 * g : 64 * (i >> 1) + 16 * g + 8 * (i & 1)));
         }
         // Rows in the caches of a step's blocks of 16 tokens (pages are whole blocks, so all 16 rows are there).  A block past the
         // end is whatever the table has there, kept inside the cache.  Pages are looked up a step ahead.
@@ -77,24 +80,30 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
         u32x4 kw[NB][KL];
         uint32_t vw[4 * NB][VW];
         f32x4 ks[NB], vs[NB];
+        uint32_t kb[NB], vb[NB][SB];  // blocks: this lane's key's scale, the scales of four tokens' values
         auto load_k = [&](int base, const int *page) {
 #pragma unroll
             for (int i = 0; i < NB; i++) {
                 const size_t r = block(base, i, page);
-                const uint8_t *p = (const uint8_t *)a.k + r * (D * BYTES) + col * (D * BYTES) + 16 * g;
+                const uint8_t *p = (const uint8_t *)a.k + r * ROW + col * ROW + KB * g;
 #pragma unroll
-                for (int j = 0; j < KL; j++) kw[i][j] = *(const u32x4 *)(p + 64 * j);
-                if constexpr (TYPE != SQP_FP16) ks[i] = *(const f32x4 *)(a.k_scales + r + 4 * g);
+                for (int j = 0; j < KL; j++) {
+                    if constexpr (KB == 16) kw[i][j] = *(const u32x4 *)(p + 64 * j);
+                    else kw[i][j].xy = *(const u32x2 *)p;
+                }
+                if constexpr (CODES) ks[i] = *(const f32x4 *)((const float *)a.k_scales + r + 4 * g);
+                if constexpr (BLOCKS) kb[i] = ((const uint8_t *)a.k_scales)[r * SB + col * SB + (D / 4 * g) / 32];
             }
         };
         auto load_v = [&](int base, const int *page) {
 #pragma unroll
             for (int i = 0; i < NB; i++) {
                 const size_t r = block(base, i, page);
-                const uint8_t *p = (const uint8_t *)a.v + r * (D * BYTES) + col * (DPL * BYTES);
+                const uint8_t *p = (const uint8_t *)a.v + r * ROW + col * VB;
 #pragma unroll
-                for (int j = 0; j < 4; j++) sqp_words<4 * VW>(p + (4 * g + j) * (D * BYTES), vw[4 * i + j]);
-                if constexpr (TYPE != SQP_FP16) vs[i] = *(const f32x4 *)(a.v_scales + r + 4 * g);
+                for (int j = 0; j < 4; j++) sqp_words<VB>(p + (4 * g + j) * ROW, vw[4 * i + j]);
+                if constexpr (CODES) vs[i] = *(const f32x4 *)((const float *)a.v_scales + r + 4 * g);
+                if constexpr (BLOCKS) sqp_words<4 * SB>((const uint8_t *)a.v_scales + r * SB + 4 * g * SB, vb[i]);
             }
         };
 
@@ -119,6 +128,11 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                 for (int j = 0; j < KL; j++) {
                     if constexpr (TYPE == SQP_FP16) {
                         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, kw[i][j]), qf[j], acc, 0, 0, 0);
+                    } else if constexpr (BLOCKS) {
+                        const float step = sqp_key_scale(kb[i]);
+                        const uint32_t w[4] = {kw[i][j].x, kw[i][j].y, kw[i][j].z, kw[i][j].w};
+#pragma unroll
+                        for (int e = 0; e < D / 32; e++) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(sqp_e2m1_halves8(w[e], step), qf[e], acc, 0, 0, 0);
                     } else {
                         const uint32_t w[4] = {kw[i][j].x, kw[i][j].y, kw[i][j].z, kw[i][j].w};
 #pragma unroll
@@ -132,7 +146,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                     }
                 }
 #pragma unroll
-                for (int r = 0; r < 4; r++) t[4 * i + r] = TYPE == SQP_FP16 ? acc[r] * a.scale2 : acc[r] * (ks[i][r] * a.scale2);
+                for (int r = 0; r < 4; r++) t[4 * i + r] = !CODES ? acc[r] * a.scale2 : acc[r] * (ks[i][r] * a.scale2);
             }
             const bool more = base + 64 * NB < hi;
             look_up(base + 128 * NB, ahead);
@@ -145,7 +159,11 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                     if (key >= s.len) {  // memory past the length, whatever it holds
 #pragma unroll
                         for (int e = 0; e < VW; e++) vw[i][e] = 0;
-                        if (TYPE != SQP_FP16) vs[i >> 2][i & 3] = 0.f;
+                        if (CODES) vs[i >> 2][i & 3] = 0.f;
+                        if constexpr (BLOCKS) {
+                            if constexpr (SB == 4) vb[i >> 2][i & 3] = 0;
+                            else vb[i >> 2][(i & 3) / 2] &= i & 1 ? 0xffffu : 0xffff0000u;
+                        }
                     }
                 }
             }
@@ -155,7 +173,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
 #pragma unroll
             for (int i = 0; i < 4 * NB; i++) {
                 float weight = t[i];
-                if constexpr (TYPE != SQP_FP16) {
+                if constexpr (CODES) {
                     weight += sqp_log_scale(vs[i >> 2][i & 3]);
                     vs[i >> 2][i & 3] = sqp_known_scale(vs[i >> 2][i & 3]);
                 }
@@ -175,7 +193,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             for (int i = 0; i < 4 * NB; i++) {
                 const float p = sqp_exp2(t[i] - m);
                 l += p;
-                const float pv = TYPE == SQP_FP16 ? p : p * vs[i >> 2][i & 3];
+                const float pv = !CODES ? p : p * vs[i >> 2][i & 3];
                 pf[i >> 3][i & 7] = (h16)pv;
                 pr[i >> 3][i & 7] = (h16)(pv - (float)pf[i >> 3][i & 7]);
             }
@@ -183,9 +201,26 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             for (int q = 0; q < NB / 2; q++) {
                 uint32_t pairs[4][DPL];  // [pair of tokens][dimension]
 #pragma unroll
-                for (int j = 0; j < 4; j++)
+                for (int j = 0; j < 4; j++) {
+                    if constexpr (BLOCKS) {
+                        // token i's scale of the block of dimensions that this lane has: byte SB (i & 3) + block of its four tokens' scales
+                        auto step = [&](int i) {
+                            const uint32_t w = SB == 4 ? vb[i >> 2][i & 3] : vb[i >> 2][(i & 3) / 2] >> (i & 1 ? 16 : 0);
+                            return sqp_value_scale(w >> (8 * (DPL * col / 32)) & 255u);
+                        };
+                        const int i = 8 * q + 2 * j;
+                        const float one = step(i), two = step(i + 1);
 #pragma unroll
-                    for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(vw[8 * q + 2 * j][e], vw[8 * q + 2 * j + 1][e], &pairs[j][e * (4 / BYTES)]);
+                        for (int e = 0; e < DPL / 2; e++) {
+                            const uint32_t x = sqp_e2m1_halves2(vw[i][0], one, e), y = sqp_e2m1_halves2(vw[i + 1][0], two, e);
+                            pairs[j][2 * e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                            pairs[j][2 * e + 1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VW; e++) sqp_pair_up<TYPE>(vw[8 * q + 2 * j][e], vw[8 * q + 2 * j + 1][e], &pairs[j][e * (4 / BYTES)]);
+                    }
+                }
                 if (more && q == NB / 2 - 1) load_v(base + 64 * NB, page);
 #pragma unroll
                 for (int d = 0; d < DPL; d++) {
@@ -266,6 +301,7 @@ void sqp_attention_few(int type, int D, const SqpAttention &a, const SqpParts &p
 #define FEW(TYPE) (D == 128 ? launch<TYPE, 128>(a, p, most_rows, slots, st) : launch<TYPE, 64>(a, p, most_rows, slots, st))
     if (type == SQP_FP16) FEW(SQP_FP16);
     else if (type == SQP_INT8) FEW(SQP_INT8);
-    else FEW(SQP_E4M3);
+    else if (type == SQP_E4M3) FEW(SQP_E4M3);
+    else FEW(SQP_E2M1);
 #undef FEW
 }

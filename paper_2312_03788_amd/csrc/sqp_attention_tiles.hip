@@ -38,15 +38,16 @@ namespace {
 template <int TYPE, int D, int W>
 __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAttention a, const SqpParts parts, int above_rows, int fold)
 {
-    constexpr bool CODES = TYPE != SQP_FP16;
-    constexpr int ROWS = 32 * W, BYTES = SqpCode<TYPE>::BYTES;
+    constexpr bool BLOCKS = TYPE == SQP_E2M1, CODES = TYPE != SQP_FP16 && !BLOCKS;  // (codes with a scale per token)
+    constexpr int ROWS = 32 * W, BYTES = TYPE == SQP_FP16 ? 2 : 1, ROW = SQP_ROW_BYTES<TYPE, D>;
+    constexpr int SB = D / 32;                      // bytes of scales per token (blocks)
     constexpr int TOKENS = 64 / W;                  // that a wave stages
-    constexpr int KU = D * BYTES / 16;              // 16-byte pieces per token of K
+    constexpr int KU = ROW / 16;                    // 16-byte pieces per token of K
     constexpr int KL = (TOKENS * KU + 63) / 64;     // of them per lane
-    constexpr int KPIECES = KL * (CODES ? 2 : 1);   // its stores
+    constexpr int KPIECES = KL * (BLOCKS ? 4 : CODES ? 2 : 1);  // its stores
     constexpr int VD = W == 4 ? D / 32 : D / 64;    // dimensions per lane of V (4 waves: half a wave holds a token, 8 waves: a wave)
     constexpr int VSUB = D / 32 / VD;               // blocks of 32 rows of V^T per dimension of a lane
-    constexpr int VB = VD * BYTES, VW = (VB + 3) / 4;
+    constexpr int VB = BLOCKS ? (VD + 1) / 2 : VD * BYTES, VW = (VB + 3) / 4;  // (blocks, one dimension per lane: a byte, and half of it)
     constexpr int NK = D / 16, NV = D / 32;         // operands per step: of K, of V per 16 tokens
     constexpr int AHEAD = CODES && W == 4 ? 3 : 4;  // operands fetched ahead (as many as the registers hold)
     constexpr int KROW = D + 8, VROW = 64 + 8;      // 16 bytes between rows: eight lanes' operands lie in eight different sets of banks
@@ -90,6 +91,9 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         };
         // ---- staging; pages are looked up a tile ahead
         uint32_t kw[4 * KL], vw[8 * VW];
+        uint32_t kb = 0, vb[2 * SB];  // blocks: the scale of this lane's piece of K, the scales of its 8 tokens' values
+#pragma unroll
+        for (int i = 0; i < 2 * SB; i++) vb[i] = 0;
         float kscale = 0.f, kvscale = 0.f, vscale = 0.f;
         auto place = [&](int base) { return min(base + 16 * block16, (hi - 1) & ~15); };
         auto look_up = [&](int base) { return lo < hi ? sqp_page(a, table, place(base)) : 0; };
@@ -100,29 +104,37 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
         auto load_k = [&](int base) {
             const size_t r = cache_row(page_k, base) + first_token;
             page_k = look_up(base + 64);
-            const uint8_t *kp = (const uint8_t *)a.k + r * (D * BYTES) + lane % (TOKENS * KU) * 16;
+            const uint8_t *kp = (const uint8_t *)a.k + r * ROW + lane % (TOKENS * KU) * 16;
 #pragma unroll
             for (int i = 0; i < KL; i++) sqp_words<16>(kp + 1024 * i, &kw[4 * i]);
             if constexpr (CODES) {
-                kscale = a.k_scales[r + lane % TOKENS];
-                kvscale = a.v_scales[r + lane % TOKENS];
+                kscale = ((const float *)a.k_scales)[r + lane % TOKENS];
+                kvscale = ((const float *)a.v_scales)[r + lane % TOKENS];
             }
+            if constexpr (BLOCKS) kb = ((const uint8_t *)a.k_scales)[r * SB + lane % (TOKENS * KU)];
         };
         auto load_v = [&](int base) {
             const size_t r = cache_row(page_v, base);
             page_v = look_up(base + 64);
-            const uint8_t *vp = (const uint8_t *)a.v + (r + 4 * v_half) * (D * BYTES) + v_lane * VB;
+            const uint8_t *vp = (const uint8_t *)a.v + (r + 4 * v_half) * ROW + (BLOCKS ? v_lane * VD / 2 : v_lane * VB);
 #pragma unroll
-            for (int j = 0; j < 8; j++) sqp_words<VB>(vp + (8 * (j >> 2) + (j & 3)) * (D * BYTES), &vw[j * VW]);
-            if constexpr (CODES) vscale = a.v_scales[r + first_token + lane % TOKENS];
+            for (int j = 0; j < 8; j++) sqp_words<VB>(vp + (8 * (j >> 2) + (j & 3)) * ROW, &vw[j * VW]);
+            if constexpr (CODES) vscale = ((const float *)a.v_scales)[r + first_token + lane % TOKENS];
+            if constexpr (BLOCKS) {
+                const uint8_t *bp = (const uint8_t *)a.v_scales + (r + 4 * v_half) * SB;
+                sqp_words<4 * SB>(bp, &vb[0]);
+                sqp_words<4 * SB>(bp + 8 * SB, &vb[SB]);
+            }
         };
         // (The empty statements keep a piece's work, and with it the wait for its loads, where the piece is.)
         auto store_k = [&](int buf, int piece) {
-            const int i = CODES ? piece / 2 : piece, unit = lane % (TOKENS * KU) + 64 * i;
+            const int i = BLOCKS ? piece / 4 : CODES ? piece / 2 : piece, unit = lane % (TOKENS * KU) + 64 * i;
 #pragma unroll
             for (int e = 0; e < 4; e++) asm volatile("" : "+v"(kw[4 * i + e]));
             h16 *to = &s_k[buf][(16 * block16 + first_token + unit / KU) * KROW];
-            if constexpr (CODES) {
+            if constexpr (BLOCKS) {
+                *(h16x8 *)&to[32 * (unit % KU) + 8 * (piece & 3)] = sqp_e2m1_halves8(kw[4 * i + (piece & 3)], sqp_key_scale(kb));
+            } else if constexpr (CODES) {
                 h16x2 p[4];
                 sqp_halves4<TYPE>(kw[4 * i + 2 * (piece & 1)], p[0], p[1]);
                 sqp_halves4<TYPE>(kw[4 * i + 2 * (piece & 1) + 1], p[2], p[3]);
@@ -143,15 +155,29 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
                     const int key = base + 16 * block16 + 8 * (j >> 2) + 4 * v_half + (j & 3);
 #pragma unroll
                     for (int e = 0; e < VW; e++) vw[j * VW + e] = key >= s.len ? 0 : vw[j * VW + e];
+                    if constexpr (BLOCKS) {
+                        if constexpr (SB == 4) vb[j] = key >= s.len ? 0 : vb[j];
+                        else vb[j / 2] &= key >= s.len ? (j & 1 ? 0xffffu : 0xffff0000u) : 0xffffffffu;
+                    }
                 }
             }
         };
         auto store_v = [&](int buf, int d) {
             u32x4 x;
 #pragma unroll
-            for (int j = 0; j < 8; j++) asm volatile("" : "+v"(vw[j * VW + d * BYTES / 4]));
+            for (int j = 0; j < 8; j++) asm volatile("" : "+v"(vw[j * VW + (BLOCKS ? 0 : d * BYTES / 4)]));
+            if constexpr (BLOCKS) {
+                auto one = [&](int j) {  // dimensions d and its neighbour of token j
+                    const uint32_t s = SB == 4 ? vb[j] : vb[j / 2] >> (j & 1 ? 16 : 0);
+                    const uint32_t w = VD == 1 ? vw[j] >> (4 * (v_lane & 1)) : vw[j];
+                    return sqp_e2m1_halves2(w, sqp_value_scale(s >> (8 * (VD * v_lane / 32)) & 255u), d / 2);
+                };
 #pragma unroll
-            for (int j = 0; j < 4; j++) x[j] = sqp_pair<TYPE>(&vw[2 * j * VW], &vw[(2 * j + 1) * VW], d);
+                for (int j = 0; j < 4; j++) x[j] = __builtin_amdgcn_perm(one(2 * j + 1), one(2 * j), d & 1 ? 0x07060302u : 0x05040100u);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++) x[j] = sqp_pair<TYPE>(&vw[2 * j * VW], &vw[(2 * j + 1) * VW], d);
+            }
             *(u32x4 *)&s_v[buf][(32 * VSUB * d + v_lane) * VROW + 16 * block16 + 8 * v_half] = x;
             if (CODES && d == VD - 1 && lane < TOKENS) s_rv[buf][16 * block16 + first_token + lane] = 1.f / fmaxf(vscale, SQP_LEAST_SCALE);
         };
@@ -299,6 +325,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
             load_q();
             uint32_t first_kw[4 * KL];
             const float first_kscale = kscale, first_kvscale = kvscale;
+            const uint32_t first_kb = kb;
 #pragma unroll
             for (int i = 0; i < 4 * KL; i++) first_kw[i] = kw[i];
             load_k(lo + 64);
@@ -312,6 +339,7 @@ __global__ void __launch_bounds__(64 * W, 2) attention_tiles_kernel(const SqpAtt
             for (int i = 0; i < 4 * KL; i++) kw[i] = first_kw[i];
             kscale = first_kscale;
             kvscale = first_kvscale;
+            kb = first_kb;
 #pragma unroll
             for (int i = 0; i < KPIECES; i++) store_k(0, i);
             load_k(lo + 128);
@@ -438,6 +466,7 @@ void sqp_attention_tiles(int type, int D, const SqpAttention &a, const SqpParts 
 #define TILES(TYPE) (D == 128 ? launch<TYPE, 128>(a, p, tile_rows, above_rows, fold, st) : launch<TYPE, 64>(a, p, tile_rows, above_rows, fold, st))
     if (type == SQP_FP16) TILES(SQP_FP16);
     else if (type == SQP_INT8) TILES(SQP_INT8);
-    else TILES(SQP_E4M3);
+    else if (type == SQP_E4M3) TILES(SQP_E4M3);
+    else TILES(SQP_E2M1);
 #undef TILES
 }

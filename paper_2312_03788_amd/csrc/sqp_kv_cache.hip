@@ -1,7 +1,7 @@
 // The paged cache of keys and values: [pages][kv_heads][page][D] in fp16, or as 8-bit codes with one fp32 scale per token and
 // head ([pages][kv_heads][page]).  Writing rotates queries and keys (positions as angles: y = x e^{i angle} on the pairs
 // (x_j, x_{j + D/2})) and quantises on the way, so that the projection's output is read once and nothing lies in memory in between.
-#include "sqp_rows.h"
+#include "sqp_mx.h"
 
 namespace {
 
@@ -11,8 +11,7 @@ struct CacheArgs {
     long q_stride, k_stride, v_stride;
     const int *slots, *positions;
     const float *cos_sin;
-    void *k_cache, *v_cache;
-    float *k_scales, *v_scales;
+    void *k_cache, *v_cache, *k_scales, *v_scales;
     h16 *q_out;
 };
 
@@ -74,6 +73,17 @@ __global__ void __launch_bounds__(256) kv_write_kernel(const CacheArgs a)
         h16 *dst = (h16 *)cache + at * D + 8 * lane;
         *(uint4 *)dst = sqp_narrow8(f);
         *(uint4 *)(dst + D / 2) = sqp_narrow8(f + 8);
+    } else if constexpr (TYPE == SQP_E2M1) {
+        // four neighbouring lanes have a block of either half of the row
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            uint32_t amax = 0;
+#pragma unroll
+            for (int j = 0; j < 8; j++) amax = max(amax, sqp_abs_bits(f[8 * half + j]));
+            const uint32_t byte = sqp_mx_byte<SQP_E2M1>(sqp_quad_max(amax));
+            ((uint32_t *)cache)[at * (D / 8) + half * (D / 16) + lane] = sqp_mx_e2m1_codes8(f + 8 * half, byte);
+            if (lane % 4 == 0) ((uint8_t *)(is_v ? a.v_scales : a.k_scales))[at * (D / 32) + half * (D / 64) + lane / 4] = (uint8_t)byte;
+        }
     } else {
         uint32_t amax = 0;
 #pragma unroll
@@ -85,15 +95,15 @@ __global__ void __launch_bounds__(256) kv_write_kernel(const CacheArgs a)
         uint8_t *dst = (uint8_t *)cache + at * D + 8 * lane;
         *(uint2 *)dst = sqp_codes8<TYPE>(f, inverse);
         *(uint2 *)(dst + D / 2) = sqp_codes8<TYPE>(f + 8, inverse);
-        if (lane == 0) (is_v ? a.v_scales : a.k_scales)[at] = step;
+        if (lane == 0) ((float *)(is_v ? a.v_scales : a.k_scales))[at] = step;
     }
 }
 
 // The same rows back as fp16: D / 8 lanes per row.
 template <int TYPE, int D>
 __global__ void __launch_bounds__(256) kv_read_kernel(int kv_heads, int page_shift, int slots_total, const int *__restrict__ slots, const void *__restrict__ k_cache,
-                                                      const void *__restrict__ v_cache, const float *__restrict__ k_scales,
-                                                      const float *__restrict__ v_scales, h16 *__restrict__ k, h16 *__restrict__ v)
+                                                      const void *__restrict__ v_cache, const void *__restrict__ k_scales,
+                                                      const void *__restrict__ v_scales, h16 *__restrict__ k, h16 *__restrict__ v)
 {
     constexpr int LANES = D / 8, ROWS = 256 / LANES;
     const int token = blockIdx.x, lane = threadIdx.x % LANES;
@@ -110,9 +120,14 @@ __global__ void __launch_bounds__(256) kv_read_kernel(int kv_heads, int page_shi
     const void *cache = is_v ? v_cache : k_cache;
     if constexpr (TYPE == SQP_FP16) {
         *dst = *(const uint4 *)((const h16 *)cache + at * D + 8 * lane);
+    } else if constexpr (TYPE == SQP_E2M1) {
+        const uint32_t byte = ((const uint8_t *)(is_v ? v_scales : k_scales))[at * (D / 32) + lane / 4];
+        float f[8];
+        sqp_mx_e2m1_values8(((const uint32_t *)cache)[at * (D / 8) + lane], __builtin_bit_cast(float, byte << 23), f);
+        *dst = sqp_narrow8(f);
     } else {
         const uint2 c = *(const uint2 *)((const uint8_t *)cache + at * D + 8 * lane);
-        const float step = (is_v ? v_scales : k_scales)[at];
+        const float step = ((const float *)(is_v ? v_scales : k_scales))[at];
         h16x2 p[4];
         sqp_halves4<TYPE>(c.x, p[0], p[1]);
         sqp_halves4<TYPE>(c.y, p[2], p[3]);
@@ -135,7 +150,7 @@ void write(int T, const CacheArgs &a, hipStream_t st)
 }
 
 template <int TYPE, int D>
-void read(int T, int kv_heads, int shift, int total, const int *slots, const void *kc, const void *vc, const float *ks, const float *vs, void *k, void *v, hipStream_t st)
+void read(int T, int kv_heads, int shift, int total, const int *slots, const void *kc, const void *vc, const void *ks, const void *vs, void *k, void *v, hipStream_t st)
 {
     const dim3 grid((unsigned)T, (unsigned)((2 * kv_heads + 2048 / D - 1) / (2048 / D)));
     kv_read_kernel<TYPE, D><<<grid, 256, 0, st>>>(kv_heads, shift, total, slots, kc, vc, ks, vs, (h16 *)k, (h16 *)v);
@@ -143,10 +158,10 @@ void read(int T, int kv_heads, int shift, int total, const int *slots, const voi
 
 }  // namespace
 
-int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const void *k_cache, const void *v_cache, const float *k_scales, const float *v_scales)
+int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const void *k_cache, const void *v_cache, const void *k_scales, const void *v_scales)
 {
     if (!k_cache || !v_cache) return SQP_ERR_NULL;
-    if (type != SQP_FP16 && type != SQP_INT8 && type != SQP_E4M3) return SQP_ERR_ARG;
+    if (type != SQP_FP16 && type != SQP_INT8 && type != SQP_E4M3 && type != SQP_E2M1) return SQP_ERR_ARG;
     if (type != SQP_FP16 && (!k_scales || !v_scales)) return SQP_ERR_NULL;
     if (kv_heads <= 0 || kv_heads > 65535 || (D != 64 && D != 128) || pages <= 0) return SQP_ERR_SHAPE;
     if (page < 16 || page > 65536 || (page & (page - 1)) || (long)pages * page >= (1L << 31) || sqp_too_big((long)kv_heads * page, D)) return SQP_ERR_SHAPE;
@@ -157,7 +172,7 @@ int sqp_check_cache(int kv_heads, int D, int type, int page, int pages, const vo
 
 extern "C" int sqp_kv_cache_write(int T, int heads, int kv_heads, int D, int type, int page, int pages, const void *q, long q_stride, const void *k,
                                   long k_stride, const void *v, long v_stride, const int *slots, const float *cos_sin, const int *positions,
-                                  int n_positions, void *k_cache, void *v_cache, float *k_scales, float *v_scales, void *q_out, void *stream)
+                                  int n_positions, void *k_cache, void *v_cache, void *k_scales, void *v_scales, void *q_out, void *stream)
 {
     const int rc = sqp_check_cache(kv_heads, D, type, page, pages, k_cache, v_cache, k_scales, v_scales);
     if (rc) return rc;
@@ -180,13 +195,14 @@ extern "C" int sqp_kv_cache_write(int T, int heads, int kv_heads, int D, int typ
 #define KV_WRITE(TYPE) (D == 128 ? write<TYPE, 128>(T, a, st) : write<TYPE, 64>(T, a, st))
     if (type == SQP_FP16) KV_WRITE(SQP_FP16);
     else if (type == SQP_INT8) KV_WRITE(SQP_INT8);
-    else KV_WRITE(SQP_E4M3);
+    else if (type == SQP_E4M3) KV_WRITE(SQP_E4M3);
+    else KV_WRITE(SQP_E2M1);
 #undef KV_WRITE
     return sqp_launch_status();
 }
 
 extern "C" int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page, int pages, const int *slots, const void *k_cache, const void *v_cache,
-                                 const float *k_scales, const float *v_scales, void *k, void *v, void *stream)
+                                 const void *k_scales, const void *v_scales, void *k, void *v, void *stream)
 {
     const int rc = sqp_check_cache(kv_heads, D, type, page, pages, k_cache, v_cache, k_scales, v_scales);
     if (rc) return rc;
@@ -201,7 +217,8 @@ extern "C" int sqp_kv_cache_read(int T, int kv_heads, int D, int type, int page,
                                 : read<TYPE, 64>(T, kv_heads, shift, pages * page, slots, k_cache, v_cache, k_scales, v_scales, k, v, st))
     if (type == SQP_FP16) KV_READ(SQP_FP16);
     else if (type == SQP_INT8) KV_READ(SQP_INT8);
-    else KV_READ(SQP_E4M3);
+    else if (type == SQP_E4M3) KV_READ(SQP_E4M3);
+    else KV_READ(SQP_E2M1);
 #undef KV_READ
     return sqp_launch_status();
 }

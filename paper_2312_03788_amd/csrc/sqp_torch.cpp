@@ -41,11 +41,17 @@ typedef int (*InterleaveFn)(int, int, const void *, const void *, void *, void *
 typedef int (*AddNormFn)(int, int, const void *, const void *, const void *, float, void *, void *, void *);
 typedef int (*AddNormQuantFn)(int, int, int, const void *, const void *, const void *, float, void *, float *, void *, void *);
 typedef int (*CacheWriteFn)(int, int, int, int, int, int, int, const void *, long, const void *, long, const void *, long, const int *, const float *,
-                            const int *, int, void *, void *, float *, float *, void *, void *);
-typedef int (*CacheReadFn)(int, int, int, int, int, int, const int *, const void *, const void *, const float *, const float *, void *, void *, void *);
-typedef int (*AttentionFn)(int, int, int, int, int, int, int, int, int, int, int, float, const void *, long, const void *, const void *, const float *,
-                           const float *, const int *, long, const int *, const int *, void *, void *, size_t, void *);
+                            const int *, int, void *, void *, void *, void *, void *, void *);
+typedef int (*CacheReadFn)(int, int, int, int, int, int, const int *, const void *, const void *, const void *, const void *, void *, void *, void *);
+typedef int (*AttentionFn)(int, int, int, int, int, int, int, int, int, int, int, float, const void *, long, const void *, const void *, const void *,
+                           const void *, const int *, long, const int *, const int *, void *, void *, size_t, void *);
 typedef size_t (*AttentionScratchFn)(int, int, int, int, int, int, int);
+typedef int (*MxQuantizeFn)(int, int, int, const void *, void *, uint8_t *, void *);
+typedef int (*MxDequantizeFn)(int, int, int, const void *, const uint8_t *, void *, void *);
+typedef int (*MxWeightFn)(int, int, const void *, void *, uint8_t *, void *);
+typedef int (*MxGemmFn)(int, int, int, int, int, const void *, const uint8_t *, const void *, const uint8_t *, void *, void *, size_t, void *);
+typedef size_t (*MxScratchFn)(int, int, int, int);
+typedef int (*AddNormMxFn)(int, int, int, const void *, const void *, const void *, float, void *, uint8_t *, void *, void *);
 
 GemmFn g_gemm[3];  // plain, fused activation, static scratch
 WorkspaceFn g_workspace_bytes, g_scratch_bytes;
@@ -63,6 +69,12 @@ CacheWriteFn g_cache_write;
 CacheReadFn g_cache_read;
 AttentionFn g_attention;
 AttentionScratchFn g_attention_scratch;
+MxQuantizeFn g_mx_quantize;
+MxDequantizeFn g_mx_dequantize;
+MxWeightFn g_mx_weight;
+MxGemmFn g_mx_gemm;
+MxScratchFn g_mx_scratch;
+AddNormMxFn g_add_norm_mx;
 
 // The tensor behind an argument if it is a dense GPU tensor of this type on device `dev`, else null.  A
 // subclass other than torch.nn.Parameter has semantics of its own (__torch_function__, the type of
@@ -463,8 +475,7 @@ const at::Tensor *tokens(PyObject *o, long dev, long &step)
 struct Cache {
     const at::Tensor *k, *v, *k_scales, *v_scales;
     int pages, kv_heads, page, D, type;
-    void *kp, *vp;
-    float *ksp, *vsp;
+    void *kp, *vp, *ksp, *vsp;
 };
 
 // The cache of four arguments: k_cache, v_cache, k_scales, v_scales.
@@ -474,7 +485,7 @@ bool cache(PyObject *const *a, long dev, Cache &c)
     const at::Tensor &t = THPVariable_Unpack(a[0]);
     if (!t.defined()) return false;
     const at::ScalarType type = t.scalar_type();
-    c.type = type == at::kHalf ? 0 : type == at::kChar ? 1 : type == at::kFloat8_e4m3fn ? 2 : -1;
+    c.type = type == at::kHalf ? 0 : type == at::kChar ? 1 : type == at::kFloat8_e4m3fn ? 2 : type == at::kByte ? 4 : -1;  // (kByte: e2m1, two to a byte)
     if (c.type < 0) return false;
     c.k = plain(a[0], type, dev);
     c.v = plain(a[1], type, dev);
@@ -482,16 +493,22 @@ bool cache(PyObject *const *a, long dev, Cache &c)
     for (int i = 0; i < 4; i++)
         if (!fits(c.k->size(i))) return false;
     c.pages = (int)c.k->size(0); c.kv_heads = (int)c.k->size(1); c.page = (int)c.k->size(2); c.D = (int)c.k->size(3);
+    if (c.type == 4) {
+        if (c.D > 64) return false;
+        c.D *= 2;
+    }
     c.kp = c.k->data_ptr();
     c.vp = c.v->data_ptr();
     c.ksp = c.vsp = nullptr;
     if (c.type == 0) return a[2] == Py_None && a[3] == Py_None;
-    c.k_scales = plain(a[2], at::kFloat, dev);
-    c.v_scales = plain(a[3], at::kFloat, dev);
-    if (!c.k_scales || !c.v_scales) return false;
-    if (!c.k_scales->sizes().equals(c.k->sizes().slice(0, 3)) || !c.v_scales->sizes().equals(c.k->sizes().slice(0, 3))) return false;
-    c.ksp = (float *)c.k_scales->data_ptr();
-    c.vsp = (float *)c.v_scales->data_ptr();
+    const at::ScalarType scale = c.type == 4 ? at::kByte : at::kFloat;  // e2m1: a byte per block of 32, else one scale per token and head
+    const long dims = c.type == 4 ? 4 : 3;
+    c.k_scales = plain(a[2], scale, dev);
+    c.v_scales = plain(a[3], scale, dev);
+    if (!c.k_scales || !c.v_scales || c.k_scales->dim() != dims || !c.v_scales->sizes().equals(c.k_scales->sizes())) return false;
+    if (!c.k_scales->sizes().slice(0, 3).equals(c.k->sizes().slice(0, 3)) || (dims == 4 && c.k_scales->size(3) != c.D / 32)) return false;
+    c.ksp = c.k_scales->data_ptr();
+    c.vsp = c.v_scales->data_ptr();
     return true;
 }
 
@@ -651,7 +668,213 @@ PyObject *bind_layer(PyObject *, PyObject *const *a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// The values per row of codes, 0 if they are none.
+const at::Tensor *mx_rows(PyObject *codes, PyObject *scales, long dev, const at::Tensor *&s, long &R, long &K, int &type)
+{
+    if (!THPVariable_CheckExact(codes)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(codes);
+    if (!t.defined()) return nullptr;
+    type = t.scalar_type() == at::kByte ? 4 : t.scalar_type() == at::kFloat8_e4m3fn ? 2 : 0;
+    const at::Tensor *c = type ? plain(codes, t.scalar_type(), dev) : nullptr;
+    s = plain(scales, at::kByte, dev);
+    if (!c || !s || c->dim() != 2 || s->dim() != 2) return nullptr;
+    R = c->size(0);
+    K = c->size(1) * (type == 4 ? 2 : 1);
+    return fits(R) && fits(K) && K % 32 == 0 && s->size(0) == R && s->size(1) == K / 32 ? c : nullptr;
+}
+
+// mx_quantize(type, x, device, stream): new (codes, scales)
+PyObject *mx_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 4 || !g_mx_quantize || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    const long type = PyLong_AsLong(a[0]);
+    if (type != 4 && type != 2) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    try {
+        const at::Tensor *x = plain(a[1], at::kHalf, dev);
+        if (!x || x->dim() != 2 || !fits(x->size(0)) || !fits(x->size(1)) || x->size(1) % 32) Py_RETURN_NONE;
+        const long R = x->size(0), K = x->size(1);
+        const at::Tensor codes = type == 4 ? fresh({R, K / 2}, at::kByte, *x) : fresh({R, K}, at::kFloat8_e4m3fn, *x), scales = fresh({R, K / 32}, at::kByte, *x);
+        const void *xp = x->data_ptr();
+        void *cp = codes.data_ptr();
+        uint8_t *sp = (uint8_t *)scales.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_mx_quantize((int)R, (int)K, (int)type, xp, cp, sp, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != 0) return PyLong_FromLong(rc);
+        return Py_BuildValue("(NN)", THPVariable_Wrap(codes), THPVariable_Wrap(scales));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// mx_quantize_weight(w, device, stream): new (codes, scales)
+PyObject *mx_quantize_weight(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 3 || !g_mx_weight || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    try {
+        const at::Tensor *w = plain(a[0], at::kHalf, dev);
+        if (!w || w->dim() != 2 || !fits(w->size(0)) || !fits(w->size(1)) || w->size(0) % 32) Py_RETURN_NONE;
+        const long K = w->size(0), N = w->size(1);
+        const at::Tensor codes = fresh({N, K / 2}, at::kByte, *w), scales = fresh({N, K / 32}, at::kByte, *w);
+        const void *wp = w->data_ptr();
+        void *cp = codes.data_ptr();
+        uint8_t *sp = (uint8_t *)scales.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_mx_weight((int)N, (int)K, wp, cp, sp, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != 0) return PyLong_FromLong(rc);
+        return Py_BuildValue("(NN)", THPVariable_Wrap(codes), THPVariable_Wrap(scales));
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// mx_dequantize(codes, scales, device, stream): new x
+PyObject *mx_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 4 || !g_mx_dequantize || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    try {
+        const at::Tensor *scales;
+        long R, K;
+        int type;
+        const at::Tensor *codes = mx_rows(a[0], a[1], dev, scales, R, K, type);
+        if (!codes) Py_RETURN_NONE;
+        const at::Tensor x = fresh({R, K}, at::kHalf, *codes);
+        const void *cp = codes->data_ptr();
+        const uint8_t *sp = (const uint8_t *)scales->data_ptr();
+        void *xp = x.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_mx_dequantize((int)R, (int)K, type, cp, sp, xp, stream);
+        Py_END_ALLOW_THREADS
+        return result(rc, Py_None, x);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// mx_gemm(silu, x, x scales, w, w scales, out, device, stream)
+PyObject *mx_gemm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 8 || !g_mx_gemm || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    const long silu = PyLong_AsLong(a[0]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    try {
+        const at::Tensor *xs, *ws;
+        long M, N, K, K2;
+        int type, w_type;
+        const at::Tensor *x = mx_rows(a[1], a[2], dev, xs, M, K, type), *w = mx_rows(a[3], a[4], dev, ws, N, K2, w_type);
+        if (!x || !w || w_type != 4 || K != K2) Py_RETURN_NONE;
+        const size_t bytes = g_mx_scratch((int)M, (int)N, (int)K, type);
+        if (bytes > 0 && a[5] != Py_None) Py_RETURN_NONE;  // (the general path looks whether the caller may not allocate)
+        const long cols = silu ? N / 2 : N;
+        at::Tensor y, scratch;
+        if (a[5] == Py_None) {
+            y = fresh({M, cols}, at::kHalf, *x);
+        } else {
+            const at::Tensor *o = plain(a[5], at::kHalf, dev);
+            if (!o || o->dim() != 2 || o->size(0) != M || o->size(1) != cols) Py_RETURN_NONE;
+            y = *o;
+        }
+        if (bytes > 0) scratch = fresh({(long)bytes}, at::kByte, *x);  // (dropped on return: whatever takes it next is ordered behind the kernels)
+        const void *xp = x->data_ptr(), *wp = w->data_ptr();
+        const uint8_t *xsp = (const uint8_t *)xs->data_ptr(), *wsp = (const uint8_t *)ws->data_ptr();
+        void *yp = y.data_ptr(), *sp = bytes > 0 ? scratch.data_ptr() : nullptr;
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_mx_gemm((int)M, (int)N, (int)K, type, (int)silu, xp, xsp, wp, wsp, yp, sp, bytes, stream);
+        Py_END_ALLOW_THREADS
+        return result(rc, a[5], y);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// add_rmsnorm_mx(type, x, residual, gamma, eps, sum out, device, stream): new (codes, scales), and the sum
+PyObject *add_rmsnorm_mx(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    long dev;
+    void *stream;
+    if (n != 8 || !g_add_norm_mx || !place(a, n, dev, stream)) Py_RETURN_NONE;
+    const long type = PyLong_AsLong(a[0]);
+    const double eps = PyFloat_AsDouble(a[4]);
+    if (PyErr_Occurred() || (type != 4 && type != 2)) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    try {
+        const at::Tensor *x = plain(a[1], at::kHalf, dev), *residual = plain(a[2], at::kHalf, dev), *gamma = plain(a[3], at::kHalf, dev);
+        if (!x || !residual || !gamma || x->dim() != 2 || !residual->sizes().equals(x->sizes()) || gamma->dim() != 1 || gamma->size(0) != x->size(1)) Py_RETURN_NONE;
+        const long M = x->size(0), H = x->size(1);
+        if (!fits(M) || !fits(H) || H % 32) Py_RETURN_NONE;
+        at::Tensor sum;
+        if (a[5] == Py_None) {
+            sum = fresh({M, H}, at::kHalf, *x);
+        } else {
+            const at::Tensor *t = plain(a[5], at::kHalf, dev);
+            if (!t || !t->sizes().equals(x->sizes())) Py_RETURN_NONE;
+            sum = *t;
+        }
+        const at::Tensor codes = type == 4 ? fresh({M, H / 2}, at::kByte, *x) : fresh({M, H}, at::kFloat8_e4m3fn, *x), scales = fresh({M, H / 32}, at::kByte, *x);
+        const void *xp = x->data_ptr(), *rp = residual->data_ptr(), *gp = gamma->data_ptr();
+        void *cp = codes.data_ptr(), *sp = sum.data_ptr();
+        uint8_t *bp = (uint8_t *)scales.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_add_norm_mx((int)M, (int)H, (int)type, xp, rp, gp, (float)eps, cp, bp, sp, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != 0) return PyLong_FromLong(rc);
+        PyObject *so = a[5];
+        if (so == Py_None) so = THPVariable_Wrap(sum);
+        else Py_INCREF(so);
+        return Py_BuildValue("(NNN)", THPVariable_Wrap(codes), THPVariable_Wrap(scales), so);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// bind_mx(addresses of sqp_mx_quantize, _dequantize, _quantize_weight, sqp_mx_gemm, _scratch_bytes, sqp_add_rmsnorm_mx)
+PyObject *bind_mx(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    void *p[6];
+    if (n != 6) {
+        PyErr_SetString(PyExc_TypeError, "bind_mx takes six addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 6; i++) p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+    g_mx_quantize = (MxQuantizeFn)p[0];
+    g_mx_dequantize = (MxDequantizeFn)p[1];
+    g_mx_weight = (MxWeightFn)p[2];
+    g_mx_gemm = (MxGemmFn)p[3];
+    g_mx_scratch = (MxScratchFn)p[4];
+    g_add_norm_mx = (AddNormMxFn)p[5];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
+    {"bind_mx", (PyCFunction)(void (*)(void))bind_mx, METH_FASTCALL, nullptr},
+    {"mx_quantize", (PyCFunction)(void (*)(void))mx_quantize, METH_FASTCALL, nullptr},
+    {"mx_quantize_weight", (PyCFunction)(void (*)(void))mx_quantize_weight, METH_FASTCALL, nullptr},
+    {"mx_dequantize", (PyCFunction)(void (*)(void))mx_dequantize, METH_FASTCALL, nullptr},
+    {"mx_gemm", (PyCFunction)(void (*)(void))mx_gemm, METH_FASTCALL, nullptr},
+    {"add_rmsnorm_mx", (PyCFunction)(void (*)(void))add_rmsnorm_mx, METH_FASTCALL, nullptr},
     {"bind_layer", (PyCFunction)(void (*)(void))bind_layer, METH_FASTCALL, nullptr},
     {"add_rmsnorm", (PyCFunction)(void (*)(void))add_rmsnorm, METH_FASTCALL, nullptr},
     {"kv_cache_write", (PyCFunction)(void (*)(void))kv_cache_write, METH_FASTCALL, nullptr},
