@@ -17,20 +17,6 @@ __device__ __forceinline__ uint32_t pick_scales(const u32x4 v, uint32_t lo, uint
     return __builtin_amdgcn_perm(v.y, v.x, lo) | __builtin_amdgcn_perm(v.w, v.z, hi);
 }
 
-// The 16 scales of blocks first .. first + 15 of a row (`left` of them are there, the others become 2^-127).
-__device__ __forceinline__ u32x4 load_scales(const uint8_t *p, int left)
-{
-    u32x4 v;
-    if (left >= 16) {
-        __builtin_memcpy(&v, p, 16);  // (rows of scales begin at any byte)
-    } else {
-        uint32_t w[4] = {0, 0, 0, 0};
-        for (int i = 0; i < left; i++) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
-        v = u32x4{w[0], w[1], w[2], w[3]};
-    }
-    return v;
-}
-
 template <int XT, int MT, int NT, int KW>
 __global__ void __launch_bounds__(64 * KW) mx_few_kernel(const SqpMxGemm a)
 {
@@ -73,7 +59,7 @@ __global__ void __launch_bounds__(64 * KW) mx_few_kernel(const SqpMxGemm a)
                 const u32x4 v = __builtin_nontemporal_load((const u32x4 *)(wp[t] + (size_t)block * 16));
                 wv[t][s] = 4 * s + g < left ? v : (u32x4)(0u);
             }
-            wsv[t] = load_scales(wsp[t] + first, left);
+            wsv[t] = sqp_mx_load_scales(wsp[t] + first, left);
         }
 #pragma unroll
         for (int t = 0; t < MT; t++) {
@@ -87,7 +73,7 @@ __global__ void __launch_bounds__(64 * KW) mx_few_kernel(const SqpMxGemm a)
                     for (int e = 0; e < 2; e++) xv[t][2 * s + e] = *(const u32x4 *)(xp[t] + (size_t)min(2 * (first + 4 * s) + 4 * e + g, 2 * blocks - 1) * 16);
                 }
             }
-            xsv[t] = load_scales(xsp[t] + first, left);
+            xsv[t] = sqp_mx_load_scales(xsp[t] + first, left);
         }
         uint32_t wsc[NT], xsc[MT];
 #pragma unroll
@@ -137,18 +123,11 @@ int pick(const SqpMxFewPlan &p, const SqpMxGemm &a, hipStream_t st)
 {
 #define FEW(MT, NT, KW) \
     if (p.mt == MT && p.nt == NT && p.kw == KW) return launch<XT, MT, NT, KW>(a, st)
-    FEW(1, 1, 4);
     FEW(1, 1, 8);
-    FEW(1, 1, 16);
-    FEW(1, 2, 4);
     FEW(1, 2, 8);
-    FEW(2, 1, 4);
     FEW(2, 1, 8);
     FEW(2, 2, 4);
-    FEW(2, 2, 8);
-    FEW(4, 1, 4);
     FEW(4, 1, 8);
-    FEW(4, 2, 4);
 #undef FEW
     return SQP_ERR_SHAPE;
 }

@@ -10,30 +10,89 @@ int g_hook_kind = 0, g_hook_a = 0, g_hook_b = 0, g_hook_c = 0;
 struct Plan {
     bool few;
     SqpMxFewPlan f;
-    SqpMxTilePlan t;
-    size_t bytes;
+    SqpMxTilePlan t;     // of the first columns
+    int cols;            // how many
+    SqpMxTilePlan rest;  // of the others (whole K), if there are any
+    size_t bytes;        // of partial sums
 };
+
+// What a call takes in us, by the number of its workgroups: the least squares over 1799 timed calls (e2m1) and 1202 (e4m3) of every tile in one
+// to eight K parts, row counts from 1 to 4096 on eight layers from 1024 x 4096 to 44032 x 8192.  A round of workgroups, as many
+// as run at once, takes `tile` and for every 512 k `chunk[n - 1]` with n workgroups on a compute unit; a joining kernel takes `join`
+// and `join_mb` per MB of partial sums; the few-rows kernel `few` and per million weights `few_w` + rows * `few_mw`.  A call is off by 11 %
+// (root mean square); over the 207 sizes the tile and parts chosen by it take 2.4 % more than the best on average, 54 % at worst (1000 x 1024 x 4096,
+// e4m3: 20.9 us in four parts, 13.6 in one), 23 % beside that one.
+struct Costs {
+    float launch, join, join_mb, few, few_w, few_mw;
+    struct {
+        float tile, chunk[4];
+        int at_once;  // per compute unit
+    } tile[SQP_MX_DIRECT_TILES];
+};
+constexpr Costs COSTS4 = {0.95f, 3.98f, 0.372f, 3.4f, 0.120f, 0.0045f,
+                          {{4.36f, {3.08f}, 1}, {3.16f, {2.28f}, 1}, {1.41f, {1.68f, 2.72f}, 2}, {1.82f, {1.33f}, 1}, {1.45f, {1.20f, 2.78f}, 2},
+                           {1.16f, {1.14f, 2.67f}, 2}, {1.17f, {0.77f, 1.30f, 2.20f, 3.24f}, 4}}};
+constexpr Costs COSTS8 = {0.49f, 3.97f, 0.358f, 3.4f, 0.130f, 0.0085f,
+                          {{6.51f, {4.06f}, 1}, {4.16f, {2.78f}, 1}, {2.24f, {1.81f, 3.54f}, 2}, {2.26f, {1.77f}, 1}, {2.53f, {1.38f}, 1},
+                           {1.69f, {1.20f, 2.82f}, 2}, {0.69f, {1.12f, 1.80f, 2.70f, 3.43f}, 4}}};
+constexpr int CUS = 256;
+
+int up(int a, int b) { return (a + b - 1) / b; }
+
+float tile_cost(const Costs &c, int t, int M, int N, int chunks, int parts)
+{
+    const auto &k = c.tile[t];
+    const int per = up(chunks, parts), real = up(chunks, per);
+    const long groups = (long)up(M, SQP_MX_TILE[t].rows) * up(N, SQP_MX_TILE[t].cols) * real, room = CUS * k.at_once;
+    const long full = groups / room, rest = groups % room;
+    float us = full * (k.tile + per * k.chunk[k.at_once - 1]);
+    if (rest) us += k.tile + per * k.chunk[up((int)rest, CUS) - 1];
+    if (real > 1) us += c.join + c.join_mb * 4e-6f * M * N * real;
+    return us + c.launch;
+}
 
 Plan plan(int M, int N, int K, int x_type, size_t room)
 {
     Plan p = {};
-    const long cus = 256;
-    const int stages = (K + (x_type == SQP_E2M1 ? 255 : 127)) / (x_type == SQP_E2M1 ? 256 : 128);
-    p.few = M <= 32;
+    p.cols = N;
+    p.t.parts = p.rest.parts = 1;
     p.f.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    p.f.nt = N >= 16384 ? 2 : 1;
-    p.f.kw = K > 2048 ? 8 : 4;
-    p.t.parts = 1;
-    if (!p.few) {
-        p.t.tile = SQP_MX_TILES - 1;
-        for (int t = 0; t < SQP_MX_TILES; t++) {
-            int rows, cols;
-            sqp_mx_tile_shape(t, &rows, &cols);
-            const long tiles = (long)((M + rows - 1) / rows) * ((N + cols - 1) / cols);
-            if (tiles >= cus * 3 / 4 || t == SQP_MX_TILES - 1 || (M > 64 && t == 1)) {
-                p.t.tile = t;
-                p.t.parts = (int)std::max(1L, std::min({2 * cus / std::max(tiles, 1L), (long)stages / 4, 16L}));
-                break;
+    p.f.nt = N >= 16384 && M <= 32 ? 2 : 1;  // (16 x 44032 x 8192: 51 us with two, 57 with one; 16 x 8192 x 8192 11.5, 11.0)
+    p.f.kw = p.f.mt == 2 && p.f.nt == 2 ? 4 : 8;
+    const int chunks = up(K, 512);
+    const size_t one = (size_t)M * N * sizeof(float);
+    const int most = (int)std::min((size_t)8, std::max(room / one, (size_t)1));
+    if (K % 128 || K < 512) {  // scales that do not begin at words, or no 16 of a row: no direct copies
+        p.few = M <= 64;
+        p.t.tile = SQP_MX_DIRECT_TILES + (M > 64 ? 0 : M > 32 ? 1 : 2);
+        const long groups = (long)up(M, 128) * up(N, 128);
+        if (!p.few) p.t.parts = (int)std::max(1L, std::min({2L * CUS / groups, (long)chunks / 2, (long)most}));
+    } else {
+        const Costs &c = x_type == SQP_E2M1 ? COSTS4 : COSTS8;
+        float best = 1e30f;
+        if (M <= 64) {
+            best = c.few + 1e-6f * N * K * (c.few_w + c.few_mw * M);
+            p.few = true;
+        }
+        auto offer = [&](int t, int parts, int cols, int rest, float us) {
+            if (us >= best) return;
+            best = us;
+            p.few = false;
+            p.t = {t, parts};
+            p.cols = cols;
+            p.rest.tile = rest;
+        };
+        const int lo = M > 96 ? 0 : M > 64 ? 1 : M > 32 ? 3 : 5, hi = M > 256 ? 3 : M > 64 ? 4 : 6;  // tiles of the rows' size
+        for (int t = lo; t <= hi; t++) {
+            const SqpMxTileShape &s = SQP_MX_TILE[t];
+            const long groups = (long)up(M, s.rows) * up(N, s.cols), at_once = CUS * c.tile[t].at_once;
+            for (int parts : {1, 2, 3, 4, 6, 8})
+                if (parts == 1 || (parts <= most && parts <= chunks && groups * parts <= at_once)) offer(t, parts, N, 0, tile_cost(c, t, M, N, chunks, parts));
+            // Whole rounds of this tile, and the columns left over in tiles of another shape.
+            if (groups > at_once && groups % at_once) {
+                const int cols = (int)(groups / at_once * at_once / up(M, s.rows)) * s.cols;
+                for (int r = t + 1; r <= hi && cols > 0 && cols < N; r++)
+                    offer(t, 1, cols, r, tile_cost(c, t, M, cols, chunks, 1) + tile_cost(c, r, M, N - cols, chunks, 1) + 1.0f);
             }
         }
     }
@@ -42,12 +101,15 @@ Plan plan(int M, int N, int K, int x_type, size_t room)
         p.f = {g_hook_a, g_hook_b, g_hook_c};
     } else if (g_hook_kind == 2) {
         p.few = false;
-        p.t = {g_hook_a, std::max(1, g_hook_b)};
+        p.t = {g_hook_a, std::min(std::max(1, g_hook_b), (int)std::min((size_t)64, std::max(room / one, (size_t)1)))};
+        p.cols = N;
+    } else if (g_hook_kind == 3) {
+        p.few = false;
+        p.t = {g_hook_a, 1};
+        p.cols = std::min(N, g_hook_c * SQP_MX_TILE[g_hook_a].cols);
+        p.rest.tile = g_hook_b;
     }
-    if (p.few) return p;
-    const size_t one = (size_t)M * N * sizeof(float);
-    if (p.t.parts > 1 && (size_t)p.t.parts * one > room) p.t.parts = (int)std::max((size_t)1, room / one);
-    p.bytes = p.t.parts > 1 ? p.t.parts * one : 0;
+    p.bytes = !p.few && p.t.parts > 1 ? p.t.parts * one : 0;
     return p;
 }
 
@@ -84,5 +146,12 @@ extern "C" int sqp_mx_gemm(int M, int N, int K, int x_type, int silu_mul, const 
     a.M = M; a.N = N; a.K = K; a.silu = silu_mul != 0;
     a.x = x; a.w = w; a.xs = x_scales; a.ws = w_scales; a.y = (h16 *)y; a.part = (float *)scratch;
     const Plan p = plan(M, N, K, x_type, scratch ? scratch_bytes : 0);
-    return p.few ? sqp_mx_few(x_type, p.f, a, (hipStream_t)stream) : sqp_mx_tiles(x_type, p.t, a, (hipStream_t)stream);
+    hipStream_t st = (hipStream_t)stream;
+    if (p.few) return sqp_mx_few(x_type, p.f, a, st);
+    a.cols = p.cols;
+    const int rc = sqp_mx_tiles(x_type, p.t, a, st);
+    if (rc || p.cols == N) return rc;
+    a.first_col = p.cols;
+    a.cols = N - p.cols;
+    return sqp_mx_tiles(x_type, p.rest, a, st);
 }

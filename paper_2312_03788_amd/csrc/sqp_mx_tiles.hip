@@ -1,13 +1,17 @@
 // Microscaled product in tiles: 32x32x64 scaled matrix instructions on operands that lie in shared memory as they do in memory.
 // Bound: the matrix cores.
 //
-// A workgroup of four waves takes BM rows x BN columns, a wave 32 RT x 32 CT of them (weights are the instruction's rows, activations
-// its columns).  K goes in stages of 128 bytes of activations (256 k of e2m1, 128 of e4m3) through two slots that are filled by direct
-// loads into shared memory, the next stage while one is consumed; pieces of 16 bytes change places within 128 bytes, so that
-// the eight rows that are read at once lie in different banks.  The order of blocks within a stage is free as long as both
-// operands and their scales have the same: of 256 k lane half h takes blocks 4 h + s in step s, so that its four scales are one word.
-// Scales come 16 bytes (512 k) of a row at a time through registers, since rows of them begin at any byte.
+// A workgroup of W = 4 or 8 waves takes BM rows x BN columns, a wave 32 RT x 32 CT of them (weights are the instruction's rows, activations
+// its columns, so that a lane's results are neighbouring columns of y).  K goes in stages of 128 bytes of activations (256 k of e2m1, 128 of
+// e4m3) through SLOTS slots, filled by direct loads into shared memory ahead of time; pieces of 16 bytes change places within 256 bytes, so
+// that the sixteen rows that are read at once lie in different banks.  Stages of 64 bytes of a row are slower (2048 x 8192 x 8192, e2m1, four
+// slots: 89 us instead of 76): every load asks for twice as many lines, and asking for them is what the loads take.
+// The order of blocks within a stage is free as long as both operands and their scales have the same: lane half h takes blocks
+// STEPS h + s in step s, so that its scales lie together.  Of e4m3 activations a lane's first 16 values belong to the lower half's block and the
+// others to the upper half's (the instruction's order).
+// Scales come 16 (512 k) of a row at a time through registers, since rows of them begin at any byte.
 #include <algorithm>
+#include <type_traits>
 
 #include "sqp_mx_gemm.h"
 
@@ -20,11 +24,21 @@ __device__ __forceinline__ rsrc_t buffer_of(const void *p, uint32_t bytes)
     return rsrc_t{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)bytes, 0x00020000};
 }
 
-// 16 bytes per lane from base + lane_offset + offset to shared memory at dst + 16 lane (beyond the buffer: zeros).  In assembly, since
-// the compiler would wait for it at the next read of shared memory; the kernel waits itself.
-__device__ __forceinline__ void copy_piece(rsrc_t base, uint32_t lane_offset, uint32_t offset, uint32_t dst)
+// 16 bytes per lane from base + (lane_offset | past) + offset to shared memory at dst + 16 lane; beyond the buffer: zeros.  In assembly, since
+// the compiler would wait for it at the next read of shared memory; the kernel waits itself.  (The address is put together between the write of
+// m0 and the load, which have to be an instruction apart.)  STREAM: with the hint for data that is read once.
+template <bool STREAM>
+__device__ __forceinline__ void copy_piece(rsrc_t base, uint32_t lane_offset, uint32_t past, uint32_t offset, uint32_t dst, uint32_t dst_more)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(dst), "v"(lane_offset), "s"(base), "s"(offset) : "memory");
+    uint32_t at;
+#define SQP_COPY_PIECE(hint)                                                                                                        \
+    asm volatile("s_add_u32 m0, %1, %2\n\tv_or_b32 %0, %3, %4\n\tbuffer_load_dwordx4 %0, %5, %6 offen " hint "lds"                \
+                 : "=&v"(at)                                                                                                        \
+                 : "s"(dst), "i"(dst_more), "v"(lane_offset), "v"(past), "s"(base), "s"(offset)                                    \
+                 : "memory", "scc")
+    if constexpr (STREAM) SQP_COPY_PIECE("nt ");
+    else SQP_COPY_PIECE("");
+#undef SQP_COPY_PIECE
 }
 
 constexpr int XCDS = 8;
@@ -36,93 +50,133 @@ __device__ __forceinline__ uint32_t xcd_run(uint32_t w, uint32_t total)
     return xcd * len + (xcd < more ? xcd : more) + w / XCDS;
 }
 
-template <int XT, int RT, int CT, int WM, int WN>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT * CT > 8 ? 1 : 2)))
-mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int stages_per_part)
+template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, bool DIRECT>
+struct Tile {
+    static constexpr bool FOUR = XT == SQP_E2M1;
+    static constexpr int BM = 32 * RT * WM, BN = 32 * CT * WN, W = WM * WN, THREADS = 64 * W;
+    static constexpr int BLOCKS = BLK, STEPS = BLOCKS / 2;              // of 32 k per stage, of two blocks
+    static constexpr int SPC = 16 / BLOCKS;                             // stages per chunk of 16 scales
+    static constexpr int XB = (FOUR ? 16 : 32) * BLOCKS, WB = 16 * BLOCKS;  // bytes of a row per stage
+    static constexpr int XCOPIES = BM * XB / 1024, COPIES = XCOPIES + BN * WB / 1024;  // of 1 KB per stage
+    static constexpr int PER = (COPIES + W - 1) / W;                    // per wave
+    static constexpr int SBM = (BM + 63) / 64 * 64;                     // rows of activations' scales (copies are of 64 rows)
+    static constexpr int STAGE = COPIES * 1024, SCALES = (SBM + BN) * 16;
+    static constexpr int SCOPIES = (SBM + BN) / 64, SPER = (SCOPIES + W - 1) / W;       // of 64 rows' scales of a chunk (DIRECT)
+    static constexpr int LDS = SLOTS * STAGE + 2 * SCALES;
+    static_assert(LDS <= 160 * 1024 && (XB < 256 || (COPIES % 4 == 0 && XCOPIES % 4 == 0 && W % 4 == 0)), "shared memory; the same piece in all of a wave's copies");
+};
+
+template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, bool DIRECT>
+__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(WM * WN == 8 || RT * CT < 8 ? 2 : 1)))
+mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int chunks_per_part)
 {
-    constexpr bool FOUR = XT == SQP_E2M1;
-    constexpr int XFMT = FOUR ? 4 : 0;
-    constexpr int BM = 32 * RT * WM, BN = 32 * CT * WN;
-    constexpr int BLOCKS = FOUR ? 8 : 4;            // of 32 k per stage
-    constexpr int STEPS = BLOCKS / 2;
-    constexpr int WB = 16 * BLOCKS;                 // bytes of a weight row per stage
-    constexpr int SPC = 16 / BLOCKS;                // stages per chunk of 16 scales
-    constexpr int XCOPIES = BM / 32, WCOPIES = BN * WB / 4096;  // copies of 1 KB per wave and stage
-    constexpr int SROWS = (BM + BN + 255) / 256;    // rows of scales per thread
-    __shared__ __attribute__((aligned(1024))) uint8_t s_x[2][BM * 128];
-    __shared__ __attribute__((aligned(1024))) uint8_t s_w[2][BN * WB];
-    __shared__ __attribute__((aligned(16))) uint8_t s_s[2][(BM + BN) * 16];
+    typedef Tile<XT, RT, CT, WM, WN, BLK, SLOTS, DIRECT> T;
+    constexpr bool FOUR = T::FOUR;
+    constexpr int XFMT = FOUR ? 4 : 0, BM = T::BM, BN = T::BN, XB = T::XB, WB = T::WB, STEPS = T::STEPS, BLOCKS = T::BLOCKS, SPC = T::SPC;
+    constexpr int AHEAD = (SLOTS - 2) * T::PER;     // copies that may be under way when the waves meet
+    constexpr int W = T::W, SROWS = (BM + BN + T::THREADS - 1) / T::THREADS;  // waves; rows of scales per thread
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::LDS];
 
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
     const int wm = wave / WN, wn = wave % WN;
-    const int blocks = a.K / SQP_MX_BLOCK, all_stages = (blocks + BLOCKS - 1) / BLOCKS;
+    const int blocks = a.K / SQP_MX_BLOCK;
     // the tile: groups of group_m rows of tiles, row index fastest
     int m0, n0;
     {
         const uint32_t i = xcd_run(blockIdx.x, gridDim.x), g = i / (uint32_t)(group_m * tiles_n), in = i - g * (uint32_t)(group_m * tiles_n);
         const uint32_t rows = min((uint32_t)group_m, (uint32_t)tiles_m - g * group_m), col = in / rows;
         m0 = (int)(g * group_m + in - col * rows) * BM;
-        n0 = (int)col * BN;
+        n0 = a.first_col + (int)col * BN;
     }
-    const int first = blockIdx.y * stages_per_part, stages = min(all_stages - first, stages_per_part);
+    const int first = blockIdx.y * chunks_per_part, end = min((blocks + 15) / 16, first + chunks_per_part);  // chunks of 512 k
 
     const uint32_t x_row = (uint32_t)a.K / (FOUR ? 2 : 1), w_row = (uint32_t)a.K / 2;
     const rsrc_t xbuf = buffer_of(a.x, (uint32_t)a.M * x_row), wbuf = buffer_of(a.w, (uint32_t)a.N * w_row);
-    // this lane's pieces: row and piece within the stage's bytes of that row
-    uint32_t xoff[XCOPIES], woff[WCOPIES];
-    int xpiece[XCOPIES], wpiece[WCOPIES];
+    const uint32_t base = (uint32_t)(size_t)&lds[0];
+    // A wave's copies: every W-th of a stage's, the activations' first (where they are no whole number of W, some are made
+    // twice, so that every wave has as many to wait for).  A copy is 4 rows of 256 bytes, 8 of 128 or 16 of 64: this lane's row and piece of it
+    // (the same in all of a wave's copies, which are even numbers of copies apart, or fours).
+    uint32_t off[T::PER];
+    auto is_x = [&](int i) { return T::XCOPIES % W == 0 && T::COPIES % W == 0 ? W * i < T::XCOPIES : (wave + W * i) % T::COPIES < T::XCOPIES; };
+    static_assert(T::XCOPIES % 2 == 0 && T::COPIES % 2 == 0, "copies of a wave are all even or all odd");
+    auto piece_of = [&](int bytes) {  // a row's pieces change places so that 256 bytes of neighbouring rows hold one piece of sixteen rows
+        return bytes == 256 ? (lane & 15) ^ (4 * (wave & 3) + (lane >> 4)) : bytes == 128 ? (lane & 7) ^ (4 * (wave & 1) + (lane >> 4)) : (lane & 3) ^ (lane >> 4);
+    };
+    const int xpiece = piece_of(XB), wpiece = piece_of(WB);
+    constexpr int XLINE = XB / 16, WLINE = WB / 16;  // pieces of a row
 #pragma unroll
-    for (int j = 0; j < XCOPIES; j++) {
-        const int row = 8 * (wave + 4 * j) + (lane >> 3);
-        xpiece[j] = (lane & 7) ^ (row & 7);
-        xoff[j] = (uint32_t)min(m0 + row, a.M - 1) * x_row + 16u * (uint32_t)xpiece[j];
+    for (int i = 0; i < T::PER; i++) {
+        const int c = (wave + W * i) % T::COPIES;
+        if (is_x(i)) off[i] = (uint32_t)min(m0 + (64 * c + lane) / XLINE, a.M - 1) * x_row + 16u * (uint32_t)xpiece;
+        else off[i] = (uint32_t)min(n0 + (64 * (c - T::XCOPIES) + lane) / WLINE, a.N - 1) * w_row + 16u * (uint32_t)wpiece;
     }
-#pragma unroll
-    for (int j = 0; j < WCOPIES; j++) {
-        int row;
-        if constexpr (FOUR) {
-            row = 8 * (wave + 4 * j) + (lane >> 3);
-            wpiece[j] = (lane & 7) ^ (row & 7);
+    // A stage's copies; pieces past the end of K are taken from beyond the buffer (no tensor has 2^31 bytes).
+    uint32_t xpast = 0, wpast = 0;
+    auto aim = [&](int stage) {
+        const int left = blocks - BLOCKS * stage;
+        xpast = xpiece < (FOUR ? left : 2 * left) ? 0u : 0x80000000u;
+        wpast = FOUR ? xpast : wpiece < left ? 0u : 0x80000000u;
+    };
+    const uint32_t wave_base = __builtin_amdgcn_readfirstlane(base + 1024u * (uint32_t)wave);
+    // Weights of calls of few rows are read by one workgroup each (64 x 44032 x 8192: 55.0 us, 52.6 with the hint); where a stage takes half of
+    // a line, the other half would be fetched again (16 rows of e4m3: 52.1, 59.5 with the hint).
+    constexpr bool STREAM = BM <= 64 && WB == 128;
+    auto copy = [&](int stage, uint32_t slot, int i) {
+        const bool x = is_x(i);
+        const uint32_t offset = (uint32_t)stage * (x ? XB : WB), past = x ? xpast : wpast;
+        if constexpr (T::COPIES % W == 0 && T::XCOPIES % W == 0) {
+            if (STREAM && !x) copy_piece<true>(wbuf, off[i], past, offset, wave_base + slot, 1024u * (uint32_t)(W * i));
+            else copy_piece<false>(x ? xbuf : wbuf, off[i], past, offset, wave_base + slot, 1024u * (uint32_t)(W * i));
         } else {
-            row = 16 * (wave + 4 * j) + (lane >> 2);
-            wpiece[j] = (lane & 3) ^ (row >> 1 & 3);
+            copy_piece<false>(x ? xbuf : wbuf, off[i], past, offset, __builtin_amdgcn_readfirstlane(base + slot + 1024u * (uint32_t)((wave + W * i) % T::COPIES)), 0u);
         }
-        woff[j] = (uint32_t)min(n0 + row, a.N - 1) * w_row + 16u * (uint32_t)wpiece[j];
+    };
+
+    // Scales, 16 blocks of every row a chunk.  A chunk that ends early is read up to its end: what is wanted lies `by` further on.
+    uint8_t *const s_s = lds + SLOTS * T::STAGE;
+    // DIRECT: copied as the codes are, since rows of them begin at words.
+    const rsrc_t xsbuf = buffer_of(a.xs, (uint32_t)a.M * (uint32_t)blocks), wsbuf = buffer_of(a.ws, (uint32_t)a.N * (uint32_t)blocks);
+    uint32_t soff[DIRECT ? T::SPER : 1];
+    auto is_xs = [&](int i) { return (wave + W * i) % T::SCOPIES < T::SBM / 64; };
+    auto copy_scales = [&](int chunk, int i) {
+        copy_piece<false>(is_xs(i) ? xsbuf : wsbuf, soff[i], 0u, (uint32_t)min(16 * chunk, blocks - 16),
+                   __builtin_amdgcn_readfirstlane(base + SLOTS * T::STAGE + (chunk & 1) * T::SCALES + 1024u * (uint32_t)((wave + W * i) % T::SCOPIES)), 0u);
+    };
+    if constexpr (DIRECT) {
+#pragma unroll
+        for (int i = 0; i < T::SPER; i++) {
+            const int row = 64 * ((wave + W * i) % T::SCOPIES) + lane;
+            soff[i] = (uint32_t)(is_xs(i) ? min(m0 + row, a.M - 1) : min(n0 + row - T::SBM, a.N - 1)) * (uint32_t)blocks;
+        }
     }
-    const uint32_t sx = (uint32_t)(size_t)&s_x[0][0], sw = (uint32_t)(size_t)&s_w[0][0];
-    auto copy_stage = [&](int t, int slot) {
-        const int st = first + t;
-        const bool whole = (st + 1) * BLOCKS <= blocks;
-        const uint32_t xat = (uint32_t)st * 128u, wat = (uint32_t)st * WB;
-        const int xleft = FOUR ? blocks - st * BLOCKS : 2 * (blocks - st * BLOCKS), wleft = blocks - st * BLOCKS;
-#pragma unroll
-        for (int j = 0; j < XCOPIES; j++)
-            copy_piece(xbuf, whole || xpiece[j] < xleft ? xoff[j] : 0xfff00000u, xat, __builtin_amdgcn_readfirstlane(sx + slot * (BM * 128) + (wave + 4 * j) * 1024));
-#pragma unroll
-        for (int j = 0; j < WCOPIES; j++)
-            copy_piece(wbuf, whole || wpiece[j] < wleft ? woff[j] : 0xfff00000u, wat, __builtin_amdgcn_readfirstlane(sw + slot * (BN * WB) + (wave + 4 * j) * 1024));
-    };
+    // Else through registers, a row or two per thread.
     u32x4 sv[SROWS];
-    auto load_scales = [&](int chunk) {  // of the whole K
-#pragma unroll
-        for (int i = 0; i < SROWS; i++) {
-            const int row = (int)threadIdx.x + 256 * i;
-            const uint8_t *p = row < BM ? a.xs + (size_t)min(m0 + row, a.M - 1) * blocks : a.ws + (size_t)min(n0 + row - BM, a.N - 1) * blocks;
-            const int at = 16 * chunk, left = blocks - at;
-            if (left >= 16) {
-                __builtin_memcpy(&sv[i], p + at, 16);
-            } else {
-                uint32_t v[4] = {0, 0, 0, 0};
-                for (int b = 0; b < left; b++) v[b >> 2] |= (uint32_t)p[at + b] << (8 * (b & 3));
-                sv[i] = u32x4{v[0], v[1], v[2], v[3]};
-            }
-        }
+    auto scale_row = [&](int i) {
+        const int row = (int)threadIdx.x + T::THREADS * i;
+        return row < BM ? a.xs + (size_t)min(m0 + row, a.M - 1) * blocks : a.ws + (size_t)min(n0 + row - BM, a.N - 1) * blocks;
     };
-    auto store_scales = [&](int chunk) {
+    auto load_first_scales = [&] {
+#pragma unroll
+        for (int i = 0; i < SROWS; i++) sv[i] = sqp_mx_load_scales(scale_row(i) + 16 * first, blocks - 16 * first);
+    };
+    // The chunks behind, without branches.  (Behind the last one something is read that is not used: the row's end, or where no row
+    // has 16 scales the activations' first bytes.)
+    const bool one_chunk = blocks < 16;
+    auto load_scales = [&](int chunk) {
+        const int at = one_chunk ? 0 : min(16 * chunk, blocks - 16);
 #pragma unroll
         for (int i = 0; i < SROWS; i++) {
-            const int row = (int)threadIdx.x + 256 * i;
-            if (row < BM + BN) *(u32x4 *)&s_s[chunk & 1][16 * row] = sv[i];
+            u32x4 v;
+            __builtin_memcpy(&v, (one_chunk ? (const uint8_t *)a.x : scale_row(i)) + at, 16);
+            sv[i] = v;
+        }
+        return 16 * chunk - at;
+    };
+    auto store_scales = [&](int chunk, int by) {
+#pragma unroll
+        for (int i = 0; i < SROWS; i++) {
+            const int row = (int)threadIdx.x + T::THREADS * i;
+            if (SROWS * T::THREADS == BM + BN || row < BM + BN) *(u32x4 *)&s_s[(chunk & 1) * T::SCALES + 16 * (row < BM ? row : row + T::SBM - BM)] = sqp_mx_shift_down(sv[i], by);
         }
     };
 
@@ -134,110 +188,177 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int st
 
     const int xr = 32 * RT * wm + l32, wr = 32 * CT * wn + l32;  // this lane's row of the wave's first tile
     u32x4 xf[2][RT][FOUR ? 1 : 2], wf[2][CT];
-    uint32_t xsc[RT], wsc[CT];
-    auto fetch = [&](int slot, int s, int to) {
+    uint32_t xsc[RT], wsc[CT], next_xsc[RT], next_wsc[CT];
+    // Operand n of a step: the weights' first, then the activations' (e4m3: two each).
+    constexpr int OPERANDS = CT + RT * (FOUR ? 1 : 2);
+    auto fetch = [&](uint32_t slot, int s, int to, int n) {
+        auto place = [](int row, int piece, int bytes) { return piece ^ (bytes == 256 ? row & 15 : bytes == 128 ? row >> 1 & 7 : row >> 2 & 3); };
+        if (n < CT) {
+            wf[to][n] = *(const u32x4 *)(lds + slot + T::XCOPIES * 1024 + (wr + 32 * n) * WB + 16 * place(wr, STEPS * h + s, WB));
+        } else {
+            const int i = FOUR ? n - CT : (n - CT) / 2, half = FOUR ? 0 : (n - CT) % 2;
+            xf[to][i][half] = *(const u32x4 *)(lds + slot + (xr + 32 * i) * XB + 16 * place(xr, FOUR ? STEPS * h + s : 2 * (STEPS * half + s) + h, XB));
+        }
+    };
+    auto fetch_scale = [&](int chunk, int u, int n) {  // of stage u of the chunk
+        int at = u * BLOCKS + STEPS * h;
+        // (a block past the end has zeros for codes, and some scale of its own row, so that no other row's NaN gets there)
+        if constexpr (DIRECT) at = min(at + max(16 * chunk - (blocks - 16), 0), 16 - STEPS);
+        const uint8_t *p = s_s + (chunk & 1) * T::SCALES + 16 * (n < CT ? T::SBM + wr + 32 * n : xr + 32 * (n - CT)) + at;
+        const uint32_t v = STEPS == 4 ? *(const uint32_t *)p : *(const uint16_t *)p;
+        if (n < CT) next_wsc[n] = v;
+        else next_xsc[n - CT] = v;
+    };
+
+    // the first stages, and the first chunk's scales
+    if constexpr (DIRECT) {
+#pragma unroll
+        for (int i = 0; i < T::SPER; i++) copy_scales(first, i);
+    }
+#pragma unroll
+    for (int t = 0; t < SLOTS - 1; t++) {
+        aim(first * SPC + t);
+#pragma unroll
+        for (int i = 0; i < T::PER; i++) copy(first * SPC + t, t * T::STAGE, i);
+        if constexpr (!DIRECT)
+            if (t == 0) {
+                load_first_scales();
+                store_scales(first, 0);
+            }
+    }
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(AHEAD) : "memory");
+#pragma unroll
+    for (int n = 0; n < CT + RT; n++) fetch_scale(first, 0, n);
+#pragma unroll
+    for (int n = 0; n < OPERANDS; n++) fetch(0, 0, 0, n);
+    constexpr int MEET = RT * CT >= 8 ? 1 : 0, LEFT = RT * CT - MEET;  // matrix instructions of a last step in front of the meeting, behind it
+    constexpr int EARLY = LEFT * T::PER / (LEFT + RT * CT);            // copies issued behind the meeting
+    aim(first * SPC + SLOTS - 1);
+#pragma unroll
+    for (int i = 0; i < EARLY; i++) copy(first * SPC + SLOTS - 1, (SLOTS - 1) * T::STAGE, i);
+
+    // The order of instructions is fixed, and there are no branches (across one the compiler moves matrix instructions).  While a step's matrix
+    // instructions run the next step's operands are fetched, and in a stage's first steps the copies of a stage to come are issued one by
+    // one into the slot of the stage before: many at once would wait for each other, and the matrix instructions behind them.  In a
+    // stage's last step, behind its first matrix instructions, the waves meet: then every read of this stage's slot has ended and the
+    // next stage has landed.  (Behind the part's last stage copies and fetches are made all the same, and not used.)
+    uint32_t slot = 0, free = (SLOTS - 1) * T::STAGE;
+    for (int c = first; c < end; c++) {
+        int by = 0;
+        if constexpr (!DIRECT) by = load_scales(c + 1);
+        auto stage = [&](auto u_) {
+            constexpr int u = decltype(u_)::value;
+            if constexpr (SLOTS == 2) {  // (known to the compiler)
+                slot = u % 2 * T::STAGE;
+                free = T::STAGE - slot;
+            }
+            const uint32_t next = slot == (SLOTS - 1) * T::STAGE ? 0u : slot + T::STAGE;
+            // (the next chunk's scales: stored where few copies are under way, since the compiler waits for all of them)
+            if constexpr (!DIRECT && SLOTS > 2 && u == SPC - 1) store_scales(c + 1, by);
+#pragma unroll
+            for (int i = 0; i < RT; i++) xsc[i] = next_xsc[i];
+#pragma unroll
+            for (int j = 0; j < CT; j++) wsc[j] = next_wsc[j];
+            auto step = [&](auto s_) {
+                constexpr int s = decltype(s_)::value;
+                constexpr bool LAST = s + 1 == STEPS;
+                constexpr int PF = (OPERANDS + (LAST ? LEFT : RT * CT) - 1) / (LAST ? LEFT : RT * CT);  // per matrix instruction: operands, scales
+                constexpr int PS = (RT + CT + LEFT - 1) / LEFT;
+                // (at a chunk's end its scales have to be there too: a stage's copies at least are younger than they)
+                constexpr int UNDER_WAY = DIRECT && SPC == 2 && u == SPC - 1 && AHEAD > T::PER ? T::PER : AHEAD;
+                if constexpr (!DIRECT && SLOTS == 2 && LAST && u == SPC - 1) store_scales(c + 1, by);
+                if constexpr (LAST) aim(c * SPC + u + SLOTS);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int q = 0; q < RT * CT; q++) {
+                    const int i = q / CT, j = q % CT;
+                    i32x8 b;
+                    if constexpr (FOUR) b = sqp_mx_operand(xf[s & 1][i][0]);
+                    else b = sqp_mx_operand(xf[s & 1][i][0], xf[s & 1][i][FOUR ? 0 : 1]);
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(sqp_mx_operand(wf[s & 1][j]), b, acc[i][j], 4, XFMT, s, (int)wsc[j], s, (int)xsc[i]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int at = LAST ? q - MEET : q;
+                    if (LAST && q == MEET) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(UNDER_WAY) : "memory");
+                    if (at >= 0) {
+#pragma unroll
+                        for (int n = at * PF; n < (at + 1) * PF; n++)
+                            if (n < OPERANDS) fetch(LAST ? next : slot, LAST ? 0 : s + 1, (s + 1) & 1, n);
+                        if constexpr (LAST) {
+#pragma unroll
+                            for (int n = at * PS; n < (at + 1) * PS; n++)
+                                if (n < RT + CT) fetch_scale(u == SPC - 1 ? c + 1 : c, (u + 1) % SPC, n);
+                        }
+                    }
+                    // the next chunk's scales
+                    if constexpr (DIRECT && u == 0 && s == 0) {
+                        if (q < T::SPER) copy_scales(c + 1, q);
+                    }
+                    // a stage's copies: behind the meeting before it, and in its first step
+                    if constexpr (LAST || s == 0) {
+                        constexpr int OVER = LEFT + RT * CT;
+                        const int p = LAST ? at : LEFT + q;
+                        if (p >= 0) {
+#pragma unroll
+                            for (int n = p * T::PER / OVER; n < (p + 1) * T::PER / OVER; n++) copy(c * SPC + u + SLOTS - (LAST ? 0 : 1), LAST ? slot : free, n);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            step(std::integral_constant<int, 0>());
+            step(std::integral_constant<int, 1>());
+            if constexpr (STEPS > 2) {
+                step(std::integral_constant<int, 2>());
+                step(std::integral_constant<int, 3>());
+            }
+            free = slot;
+            slot = next;
+        };
+        stage(std::integral_constant<int, 0>());
+        stage(std::integral_constant<int, 1>());
+        if constexpr (SPC > 2) {
+            stage(std::integral_constant<int, 2>());
+            stage(std::integral_constant<int, 3>());
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");  // (no copy may arrive any more: the slots are used again below)
+
+    // result register r of tile (i, j): row 32 i + l32, columns 32 j + 8 (r >> 2) + 4 h + (r & 3)
+    if (a.part) {
 #pragma unroll
         for (int i = 0; i < RT; i++) {
-            const int row = xr + 32 * i;
-            const uint8_t *p = &s_x[slot][row * 128];
-            if constexpr (FOUR) {
-                xf[to][i][0] = *(const u32x4 *)(p + 16 * ((4 * h + s) ^ (row & 7)));
-            } else {  // the lane's first 16 values belong to block s, the others to block 2 + s
-                xf[to][i][0] = *(const u32x4 *)(p + 16 * ((2 * s + h) ^ (row & 7)));
-                xf[to][i][FOUR ? 0 : 1] = *(const u32x4 *)(p + 16 * ((4 + 2 * s + h) ^ (row & 7)));
-            }
-        }
+            const int m = m0 + xr + 32 * i;
 #pragma unroll
-        for (int j = 0; j < CT; j++) {
-            const int row = wr + 32 * j;
-            const uint8_t *p = &s_w[slot][row * WB];
-            if constexpr (FOUR) wf[to][j] = *(const u32x4 *)(p + 16 * ((4 * h + s) ^ (row & 7)));
-            else wf[to][j] = *(const u32x4 *)(p + 16 * ((2 * h + s) ^ (row >> 1 & 3)));
-        }
-    };
-    auto fetch_scales = [&](int t) {
-        const int st = first + t;
-        const uint8_t *p = &s_s[(st / SPC) & 1][(st % SPC) * BLOCKS + (FOUR ? 4 : 2) * h];
+            for (int j = 0; j < CT; j++)
 #pragma unroll
-        for (int i = 0; i < RT; i++) xsc[i] = FOUR ? *(const uint32_t *)(p + 16 * (xr + 32 * i)) : *(const uint16_t *)(p + 16 * (xr + 32 * i));
-#pragma unroll
-        for (int j = 0; j < CT; j++) wsc[j] = FOUR ? *(const uint32_t *)(p + 16 * (BM + wr + 32 * j)) : *(const uint16_t *)(p + 16 * (BM + wr + 32 * j));
-    };
-#define SQP_MX_MFMA(s)                                                                                                                          \
-    _Pragma("unroll") for (int i = 0; i < RT; i++)                                                                                              \
-    {                                                                                                                                           \
-        i32x8 b;                                                                                                                                \
-        if constexpr (FOUR) b = sqp_mx_operand(xf[(s) & 1][i][0]);                                                                              \
-        else b = sqp_mx_operand(xf[(s) & 1][i][0], xf[(s) & 1][i][FOUR ? 0 : 1]);                                                               \
-        _Pragma("unroll") for (int j = 0; j < CT; j++) acc[i][j] =                                                                              \
-            __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(sqp_mx_operand(wf[(s) & 1][j]), b, acc[i][j], 4, XFMT, s, (int)wsc[j], s, (int)xsc[i]); \
-    }
-
-    // the first stage, and the first chunk's scales
-    copy_stage(0, 0);
-    load_scales(first / SPC);
-    store_scales(first / SPC);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (stages > 1) copy_stage(1, 1);
-    if ((first + 1) % SPC == 0 || SPC == 1 || first % SPC == 0) {}
-    fetch_scales(0);
-    fetch(0, 0, 0);
-    for (int t = 0; t < stages; t++) {
-        const int slot = t & 1, st = first + t;
-        // scales of the next chunk: on their way while the chunk's last stage is consumed
-        const bool turn = (st + 1) % SPC == 0 && t + 1 < stages;
-        if (turn) load_scales((st + 1) / SPC);
-#pragma unroll
-        for (int s = 0; s < STEPS; s++) {
-            if (s + 1 < STEPS) {
-                fetch(slot, s + 1, (s + 1) & 1);
-                if (s == 0) { SQP_MX_MFMA(0) }
-                if constexpr (STEPS > 2) {
-                    if (s == 1) { SQP_MX_MFMA(1) }
-                    if (s == 2) { SQP_MX_MFMA(2) }
+                for (int r4 = 0; r4 < 4; r4++) {
+                    const int n = n0 + 32 * CT * wn + 32 * j + 8 * r4 + 4 * h;
+                    if (m < a.M && n < a.N)
+                        *(f32x4 *)(a.part + ((size_t)blockIdx.y * a.M + m) * a.N + n) = f32x4{acc[i][j][4 * r4], acc[i][j][4 * r4 + 1], acc[i][j][4 * r4 + 2], acc[i][j][4 * r4 + 3]};
                 }
-            } else {
-                uint32_t keep_x[RT], keep_w[CT];
-#pragma unroll
-                for (int i = 0; i < RT; i++) keep_x[i] = xsc[i];
-#pragma unroll
-                for (int j = 0; j < CT; j++) keep_w[j] = wsc[j];
-                if (t + 1 < stages) {
-                    if (turn) store_scales((st + 1) / SPC);
-                    // every read of this slot has ended, the next stage has landed
-                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                    if (t + 2 < stages) copy_stage(t + 2, slot);
-                    fetch_scales(t + 1);
-                    fetch(slot ^ 1, 0, 0);
-                }
-                uint32_t next_x[RT], next_w[CT];
-#pragma unroll
-                for (int i = 0; i < RT; i++) { next_x[i] = xsc[i]; xsc[i] = keep_x[i]; }
-#pragma unroll
-                for (int j = 0; j < CT; j++) { next_w[j] = wsc[j]; wsc[j] = keep_w[j]; }
-                if constexpr (STEPS > 2) { SQP_MX_MFMA(3) } else { SQP_MX_MFMA(1) }
-#pragma unroll
-                for (int i = 0; i < RT; i++) xsc[i] = next_x[i];
-#pragma unroll
-                for (int j = 0; j < CT; j++) wsc[j] = next_w[j];
-            }
         }
+        return;
     }
-    // result register r of tile (i, j): row 32 i + l32, columns 32 j + 8 (r >> 2) + 4 h + (r & 3)
+    // Through shared memory (a wave's own part of it), so that rows leave in pieces of 16 bytes side by side.
+    const int cols = 32 * CT >> a.silu, pitch = 2 * 32 * CT + 16;
+    uint8_t *const mine = lds + wave * 32 * pitch;
+    const int out_n = a.N >> a.silu, n_first = (n0 + 32 * CT * wn) >> a.silu;
 #pragma unroll
     for (int i = 0; i < RT; i++) {
-        const int m = m0 + xr + 32 * i;
-        if (m >= a.M) continue;
 #pragma unroll
         for (int j = 0; j < CT; j++)
 #pragma unroll
             for (int r4 = 0; r4 < 4; r4++) {
-                const int n = n0 + 32 * CT * wn + 32 * j + 8 * r4 + 4 * h;
-                if (n >= a.N) continue;
                 const f32x4 v = {acc[i][j][4 * r4], acc[i][j][4 * r4 + 1], acc[i][j][4 * r4 + 2], acc[i][j][4 * r4 + 3]};
-                if (a.part) *(f32x4 *)(a.part + ((size_t)blockIdx.y * a.M + m) * a.N + n) = v;
-                else sqp_mx_store4(a, m, n, v);
+                const int col = 32 * j + 8 * r4 + 4 * h;
+                if (a.silu) *(uint32_t *)(mine + l32 * pitch + col) = sqp_half2(sqp_silu(v.x) * v.y, sqp_silu(v.z) * v.w);
+                else *(uint2 *)(mine + l32 * pitch + 2 * col) = make_uint2(sqp_half2(v.x, v.y), sqp_half2(v.z, v.w));
             }
+        for (int u = lane; u < 4 * cols; u += 64) {  // 32 rows of cols / 8 pieces
+            const int row = u / (cols / 8), p = u % (cols / 8), m = m0 + 32 * RT * wm + 32 * i + row, n = n_first + 8 * p;
+            const uint4 v = *(const uint4 *)(mine + row * pitch + 16 * p);
+            if (m < a.M && n < out_n) *(uint4 *)(a.y + (size_t)m * out_n + n) = v;
+        }
     }
 }
 
@@ -251,21 +372,18 @@ __global__ void __launch_bounds__(256) mx_join_kernel(const SqpMxGemm a, int par
     sqp_mx_store4(a, (int)(i / n4), 4 * (int)(i % n4), s);
 }
 
-struct Shape {
-    int rows, cols;
-};
-constexpr Shape SHAPES[SQP_MX_TILES] = {{256, 256}, {128, 128}, {64, 128}, {32, 128}};
-
-template <int XT, int RT, int CT, int WM, int WN>
+template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, bool DIRECT>
 int launch(const SqpMxTilePlan &p, const SqpMxGemm &a, hipStream_t st)
 {
-    constexpr int BM = 32 * RT * WM, BN = 32 * CT * WN, BLOCKS = XT == SQP_E2M1 ? 8 : 4;
-    const int tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-    const int stages = (a.K / SQP_MX_BLOCK + BLOCKS - 1) / BLOCKS, per = (stages + p.parts - 1) / p.parts, parts = (stages + per - 1) / per;
+    typedef Tile<XT, RT, CT, WM, WN, BLK, SLOTS, DIRECT> T;
+    if (DIRECT && (a.K % 128 || a.K < 512)) return SQP_ERR_SHAPE;  // (the plan takes another tile)
+    const int tm = (a.M + T::BM - 1) / T::BM, tn = (a.cols + T::BN - 1) / T::BN;
+    const int chunks = (a.K + 511) / 512, per = (chunks + p.parts - 1) / p.parts, parts = (chunks + per - 1) / per;
     if ((long)tm * tn > 0x7fffffffL || parts > 65535) return SQP_ERR_SHAPE;
     SqpMxGemm b = a;
     if (parts == 1) b.part = nullptr;
-    mx_tiles_kernel<XT, RT, CT, WM, WN><<<dim3((unsigned)(tm * tn), (unsigned)parts), 256, 0, st>>>(b, tm, tn, std::min(tm, 4), per);
+    const dim3 grid((unsigned)(tm * tn), (unsigned)parts);
+    mx_tiles_kernel<XT, RT, CT, WM, WN, BLK, SLOTS, DIRECT><<<grid, T::THREADS, 0, st>>>(b, tm, tn, std::min(tm, 4), per);
     if (parts > 1) mx_join_kernel<<<(unsigned)(((long)a.M * (a.N / 4) + 255) / 256), 256, 0, st>>>(b, parts);
     return sqp_launch_status();
 }
@@ -273,22 +391,26 @@ int launch(const SqpMxTilePlan &p, const SqpMxGemm &a, hipStream_t st)
 template <int XT>
 int pick(const SqpMxTilePlan &p, const SqpMxGemm &a, hipStream_t st)
 {
-    switch (p.tile) {
-        case 0: return launch<XT, 4, 4, 2, 2>(p, a, st);
-        case 1: return launch<XT, 2, 2, 2, 2>(p, a, st);
-        case 2: return launch<XT, 2, 1, 1, 4>(p, a, st);
-        case 3: return launch<XT, 1, 1, 1, 4>(p, a, st);
-    }
+    constexpr bool FOUR = XT == SQP_E2M1;
+    // (waves' tiles, waves; blocks per stage of e4m3 activations; slots for either type)
+#define TILE(i, RT, CT, WM, WN, BLK8, SLOTS4, SLOTS8, DIRECT)                                                                                    \
+    static_assert(SQP_MX_TILE[i].rows == 32 * RT * WM && SQP_MX_TILE[i].cols == 32 * CT * WN && SQP_MX_TILE[i].direct == DIRECT, "the tile's shape"); \
+    if (p.tile == i) return launch<XT, RT, CT, WM, WN, FOUR ? 8 : BLK8, FOUR ? SLOTS4 : SLOTS8, DIRECT>(p, a, st)
+    TILE(0, 4, 2, 2, 4, 4, 2, 3, true);
+    TILE(1, 2, 4, 2, 2, 4, 3, 4, true);
+    TILE(2, 2, 2, 2, 2, 4, 2, 3, true);
+    TILE(3, 2, 2, 2, 2, 4, 4, 5, true);
+    TILE(4, 2, 1, 1, 4, 8, 3, 4, true);
+    TILE(5, 1, 1, 1, 4, 8, 3, 3, true);
+    TILE(6, 1, 1, 1, 2, 4, 3, 3, true);
+    TILE(7, 2, 2, 2, 2, 4, 2, 3, false);
+    TILE(8, 2, 1, 1, 4, 4, 2, 2, false);
+    TILE(9, 1, 1, 1, 4, 4, 2, 2, false);
+#undef TILE
     return SQP_ERR_SHAPE;
 }
 
 }  // namespace
-
-void sqp_mx_tile_shape(int tile, int *rows, int *cols)
-{
-    *rows = SHAPES[tile].rows;
-    *cols = SHAPES[tile].cols;
-}
 
 int sqp_mx_tiles(int x_type, const SqpMxTilePlan &p, const SqpMxGemm &a, hipStream_t st)
 {

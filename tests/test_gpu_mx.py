@@ -167,7 +167,7 @@ def test_product(sqp, M, N, K, kind, silu):
     assert f(*dev, out=out) is out and torch.equal(out, y)
 
 
-FEW = [(1, 1, 4), (1, 1, 8), (1, 1, 16), (1, 2, 4), (1, 2, 8), (2, 1, 4), (2, 1, 8), (2, 2, 4), (2, 2, 8), (4, 1, 4), (4, 1, 8), (4, 2, 4)]
+FEW = [(1, 1, 8), (1, 2, 8), (2, 1, 8), (2, 2, 4), (4, 1, 8)]
 
 
 @pytest.mark.parametrize("kind", ["e2m1", "e4m3"])
@@ -182,16 +182,21 @@ def test_product_few_rows_plans(sqp, plan, M, N, K, kind):
         _check_product(sqp.mx_gemm(*dev), *ops, kind, False)
 
 
-TILES = range(4)
+TILES = {t: t not in (7, 8, 9) for t in range(10)}  # whether it is for K of whole 128 alone, 512 at least
 
 
 @pytest.mark.parametrize("kind", ["e2m1", "e4m3"])
-@pytest.mark.parametrize("M,N,K", [(40, 72, 32), (70, 136, 256), (300, 328, 1568), (270, 264, 4224)])
+@pytest.mark.parametrize("M,N,K", [(40, 72, 32), (70, 136, 256), (300, 336, 1568), (270, 272, 4224), (20, 272, 512), (140, 528, 1920)])
 def test_product_tile_plans(sqp, plan, M, N, K, kind):
     """Every tile, whole and in K parts, the parts' borders inside a chunk of 16 scales too."""
     ops = _operands(M, N, K, kind, 6)
     dev = _on_gpu(*ops, kind)
-    for tile in TILES:
+    for tile, direct in TILES.items():
+        if direct and (K % 128 or K < 512):
+            plan(2, tile, 1, 0)
+            with pytest.raises(sqp.SqpError):
+                sqp.mx_gemm(*dev)
+            continue
         for parts in (1, 2, 3, 5):
             print("case tiles", M, N, K, kind, tile, parts, flush=True)
             plan(2, tile, parts, 0)
@@ -200,6 +205,34 @@ def test_product_tile_plans(sqp, plan, M, N, K, kind):
             if parts in (1, 3):
                 _check_product(sqp.mx_gemm_silu_mul(*dev), *ops, kind, True) if N % 16 == 0 else None
             assert torch.equal(sqp.mx_gemm(*dev), y)
+
+
+@pytest.mark.parametrize("kind", ["e2m1", "e4m3"])
+@pytest.mark.parametrize("silu", [False, True])
+def test_product_columns_in_two_launches(sqp, plan, kind, silu):
+    """The first columns in tiles of one shape, the others in another's: every column once, the same values as in one launch."""
+    M, N, K = 200, 656, 1152
+    ops = _operands(M, N, K, kind, 9)
+    dev = _on_gpu(*ops, kind)
+    f = sqp.mx_gemm_silu_mul if silu else sqp.mx_gemm
+    for first, other, cols in ((0, 1, 1), (0, 3, 2), (1, 4, 2), (2, 4, 4), (1, 2, 1), (0, 2, 5)):
+        print("case two launches", kind, silu, first, other, cols, flush=True)
+        plan(3, first, other, cols)
+        _check_product(f(*dev), *ops, kind, silu)
+
+
+@pytest.mark.parametrize("M,N,K,kind", [(1, 1024, 4096, "e2m1"), (16, 4096, 2048, "e4m3"), (40, 8192, 1024, "e2m1"), (100, 2048, 8192, "e2m1"), (260, 16640, 512, "e4m3"),
+                                        (520, 10240, 512, "e2m1"), (48, 512, 8320, "e4m3"), (70, 264, 4128, "e2m1")])
+def test_product_automatic_plans(sqp, M, N, K, kind):
+    """What the library chooses by itself, over sizes that lead to each kernel, K parts and two launches: two rows against 64 bits, all of them
+    against another plan within the tolerance of both."""
+    print("case automatic", M, N, K, kind, flush=True)
+    ops = _operands(M, N, K, kind, 10)
+    dev = _on_gpu(*ops, kind)
+    y = sqp.mx_gemm(*dev)
+    rows = sorted({0, M // 2, M - 1})
+    _check_product(y[rows], ops[0][rows], ops[1][rows], ops[2], ops[3], kind, False)
+    assert torch.equal(sqp.mx_gemm(*dev), y)
 
 
 @pytest.mark.parametrize("kind", ["e2m1", "e4m3"])
