@@ -75,10 +75,10 @@ template <int TYPE, int D> constexpr int SQP_ROW_BYTES = D * (TYPE == SQP_FP16 ?
 
 // e2m1 blocks become fp16 values on their way to the matrix cores, which then work as over an fp16 cache: keys half their size (a
 // rotated key of fp16 parts reaches 92640, its block 6 x 2^14; the scores' factor makes up for it), values as they are.  What is below
-// fp16's smallest step is rounded as in an fp16 cache.  A block too large for fp16, which only values of 57344 on make, or keys that no
-// fp16 pair does, becomes NaN, and the rows that see it are computed one by one.
+// fp16's smallest step is rounded as in an fp16 cache.  A value too large for fp16 (57344 and more) becomes infinite, a key that no fp16
+// pair makes NaN (an infinite score below zero would not show), and the rows that see it are computed one by one.
 __device__ __forceinline__ float sqp_key_scale(uint32_t byte) { return __builtin_bit_cast(float, byte > 141u ? 0x7f800000u : (max(byte, 1u) - 1u) << 23); }
-__device__ __forceinline__ float sqp_value_scale(uint32_t byte) { return __builtin_bit_cast(float, byte > 140u ? 0x7f800000u : byte << 23); }
+__device__ __forceinline__ float sqp_value_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // Eight codes of a word in fp16 (a scale that is not finite makes NaN of them).
 __device__ __forceinline__ h16x8 sqp_e2m1_halves8(uint32_t w, float scale)

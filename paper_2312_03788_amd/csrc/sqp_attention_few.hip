@@ -16,11 +16,15 @@
 // The matrix cores wait for memory here, so p goes through them twice: rounded to fp16, and what that leaves, in fp16 again (2^-22
 // of p then, or 2^-35 of the row's largest where that is more).  The output's rounding is the only one left: the error of the 32
 // sequences' outputs below is 2.1e-4 of them instead of 2.6e-4, in the same time (149.2 us and 149.4); over codes it costs up to 3 % (16
-// sequences 39.0 us instead of 38.3, called again and again on the same cache).
+// sequences 39.0 us instead of 38.3, called again and again on the same cache).  Over e2m1 blocks the vector units are busy more than half of the
+// time (their conversions), so p is rounded once there: 16 sequences 26.1 us instead of 28.8, the 32 sequences 46.0 instead of 48.5.
 //
 // Measured, kernel alone: those 800 MB in 149 us (5.4 TB/s; a streaming read alone reaches 5.9 on this chip); one sequence of 32000
 // tokens, 40 heads, int8, 338 MB in 61 us (5.5 TB/s); 16 at up to 8192, 8 cached heads, e4m3, 166 MB in 36 us (4.6 TB/s, parts of unequal
-// length).  32 heads over 129 tokens: 6.1 us, the chain length, page, K, V.
+// length).  32 heads over 129 tokens: 6.1 us, the chain length, page, K, V.  The same over e2m1 blocks, calls in a row, joining included: 226 MB in
+// 46 us, 174 MB in 39 (37 alone), 86 MB in 26: bound by conversions (540 vector instructions per wave and 64 tokens before p was
+// rounded once, 430 since) and the ragged parts.  32 tokens per step and three workgroups per compute unit: 27.6 us for the 16
+// sequences, 37.8 for the long one; code for four (128 registers) spills (67 us).
 #include "sqp_attention.h"
 
 namespace {
@@ -146,7 +150,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                     }
                 }
 #pragma unroll
-                for (int r = 0; r < 4; r++) t[4 * i + r] = !CODES ? acc[r] * a.scale2 : acc[r] * (ks[i][r] * a.scale2);
+                for (int r = 0; r < 4; r++) t[4 * i + r] = BLOCKS ? acc[r] : !CODES ? acc[r] * a.scale2 : acc[r] * (ks[i][r] * a.scale2);  // (blocks: scaled as p is formed)
             }
             const bool more = base + 64 * NB < hi;
             look_up(base + 128 * NB, ahead);
@@ -179,6 +183,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                 }
                 top = i == 0 ? weight : fmaxf(top, weight);
             }
+            if constexpr (BLOCKS) top *= a.scale2;
             if (__any(top > m + SQP_WEIGHT_MOST)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -191,11 +196,11 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             h16x8 pf[NB / 2], pr[NB / 2];  // p to fp16's 11 bits, and to the next 11
 #pragma unroll
             for (int i = 0; i < 4 * NB; i++) {
-                const float p = sqp_exp2(t[i] - m);
+                const float p = sqp_exp2(BLOCKS ? __builtin_fmaf(t[i], a.scale2, -m) : t[i] - m);
                 l += p;
                 const float pv = !CODES ? p : p * vs[i >> 2][i & 3];
                 pf[i >> 3][i & 7] = (h16)pv;
-                pr[i >> 3][i & 7] = (h16)(pv - (float)pf[i >> 3][i & 7]);
+                if constexpr (!BLOCKS) pr[i >> 3][i & 7] = (h16)(pv - (float)pf[i >> 3][i & 7]);
             }
 #pragma unroll
             for (int q = 0; q < NB / 2; q++) {
@@ -226,7 +231,7 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
                 for (int d = 0; d < DPL; d++) {
                     const u32x4 x = {pairs[0][d], pairs[1][d], pairs[2][d], pairs[3][d]};
                     o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, x), pf[q], o[d], 0, 0, 0);
-                    o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, x), pr[q], o[d], 0, 0, 0);
+                    if constexpr (!BLOCKS) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, x), pr[q], o[d], 0, 0, 0);
                 }
             }
 #pragma unroll

@@ -5,7 +5,8 @@
 namespace {
 
 // A thread takes eight values, four neighbouring lanes a block: 16-byte loads, whole lines of codes.  K is a multiple of 32, so
-// blocks follow each other through the whole tensor and the rows do not matter.
+// blocks follow each other through the whole tensor and the rows do not matter.  Bound: HBM; 2048 x 8192 into e4m3 10.3 us, 51 MB, 4.9 TB/s (called
+// in a row; 1001 x 5120 4.8), back from e2m1 10240 x 8192 35 us, 212 MB, 6.1 TB/s.
 template <int TYPE>
 __global__ void __launch_bounds__(256) mx_quantize_kernel(long pieces, const uint4 *__restrict__ x, void *__restrict__ codes, uint8_t *__restrict__ scales)
 {
@@ -49,39 +50,43 @@ __global__ void __launch_bounds__(256) mx_dequantize_kernel(long pieces, const v
     x[i] = sqp_narrow8(f);
 }
 
-// A weight w [K][N] into blocks along K, one row of codes per column: codes [N][K / 2], scales [N][K / 32].  A workgroup takes 64
-// columns by 256 k; a thread two columns by a block (32 loads of 4 bytes: lines of 128 bytes over 32 lanes), and the codes change
-// places through shared memory, so that 128 bytes of a column leave together.
+// A weight w [K][N] into blocks along K, one row of codes per column: codes [N][K / 2], scales [N][K / 32].  A workgroup takes 128
+// columns by 256 k; a thread four columns by a block (32 loads of 8 bytes: 256 bytes of a row over 32 lanes), and the codes change
+// places through shared memory, so that 128 bytes of a column leave together.  10240 x 8192: 42 us, 212 MB, 5.0 TB/s (64 columns, 4 bytes
+// per load: 49).
 __global__ void __launch_bounds__(256) mx_quantize_weight_kernel(int N, int K, const h16 *__restrict__ w, uint4 *__restrict__ codes, uint8_t *__restrict__ scales)
 {
-    __shared__ uint4 s_codes[64][9];
-    __shared__ uint8_t s_scales[64][8];
-    const int pair = threadIdx.x & 31, kb = threadIdx.x >> 5, blocks = K / SQP_MX_BLOCK;
-    const int n0 = blockIdx.x * 64, kb0 = blockIdx.y * 8, n = n0 + 2 * pair;
+    constexpr int COLS = 128;
+    __shared__ uint4 s_codes[COLS][9];
+    __shared__ uint8_t s_scales[COLS][8];
+    const int quad = threadIdx.x & 31, kb = threadIdx.x >> 5, blocks = K / SQP_MX_BLOCK;
+    const int n0 = blockIdx.x * COLS, kb0 = blockIdx.y * 8, n = n0 + 4 * quad;
     if (n < N && kb0 + kb < blocks) {
         const h16 *p = w + (size_t)(kb0 + kb) * SQP_MX_BLOCK * N + n;
-        uint32_t v[32];
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        u32x2 v[32];
 #pragma unroll
-        for (int j = 0; j < 32; j++) v[j] = *(const uint32_t *)(p + (size_t)j * N);
+        for (int j = 0; j < 32; j++) v[j] = __builtin_nontemporal_load((const u32x2 *)(p + (size_t)j * N));
 #pragma unroll
-        for (int c = 0; c < 2; c++) {
+        for (int c = 0; c < 4; c++) {
             float f[32];
             uint32_t amax = 0;
 #pragma unroll
             for (int j = 0; j < 32; j++) {
-                const h16x2 both = __builtin_bit_cast(h16x2, v[j]);
-                f[j] = c ? (float)both.y : (float)both.x;
+                const uint32_t word = c >> 1 ? v[j].y : v[j].x;
+                const h16x2 both = __builtin_bit_cast(h16x2, word);
+                f[j] = c & 1 ? (float)both.y : (float)both.x;
                 amax = max(amax, sqp_abs_bits(f[j]));
             }
             const uint32_t byte = sqp_mx_byte<SQP_E2M1>(amax);
-            s_codes[2 * pair + c][kb] = make_uint4(sqp_mx_e2m1_codes8(f, byte), sqp_mx_e2m1_codes8(f + 8, byte), sqp_mx_e2m1_codes8(f + 16, byte),
+            s_codes[4 * quad + c][kb] = make_uint4(sqp_mx_e2m1_codes8(f, byte), sqp_mx_e2m1_codes8(f + 8, byte), sqp_mx_e2m1_codes8(f + 16, byte),
                                                    sqp_mx_e2m1_codes8(f + 24, byte));
-            s_scales[2 * pair + c][kb] = (uint8_t)byte;
+            s_scales[4 * quad + c][kb] = (uint8_t)byte;
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
+    for (int i = 0; i < COLS / 32; i++) {
         const int unit = threadIdx.x + 256 * i, col = unit >> 3, b = unit & 7;
         if (n0 + col < N && kb0 + b < blocks) {
             codes[(size_t)(n0 + col) * blocks + kb0 + b] = s_codes[col][b];
@@ -93,7 +98,7 @@ __global__ void __launch_bounds__(256) mx_quantize_weight_kernel(int N, int K, c
 // ---------------------------------------------------------------- residual, norm, blocks
 
 // z = r gamma / sqrt(mean r^2 + eps) is taken in 64 bits: a 32-bit z would put one in some millions of values on the other side of a border
-// between two codes, and two codes are up to a half of the value apart.  Of the double only what decides is kept: its 20 leading
+// between two codes, and two codes are up to a half of the value apart; at 2^-45 it is one in 2^40.  Of the double only what decides is kept: its 20 leading
 // mantissa bits, and whether anything is behind them, as the lowest bit of a float (all borders have four mantissa bits at most).
 __device__ __forceinline__ float mx_sticky(double z)
 {
@@ -125,10 +130,22 @@ __device__ __forceinline__ double mx_sum(double ss, double *red)
     for (int off = 32; off >= 1; off >>= 1) ss += __shfl_xor(ss, off, 64);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
     __syncthreads();
-    double all = 0.0;
+    double part[W];
 #pragma unroll
-    for (int i = 0; i < W; i++) all += red[i];
-    return all;
+    for (int i = 0; i < W; i++) part[i] = red[i];
+#pragma unroll
+    for (int half = W / 2; half >= 1; half >>= 1)
+#pragma unroll
+        for (int i = 0; i < half; i++) part[i] = part[2 * i] + part[2 * i + 1];
+    return part[0];
+}
+
+// 1 / sqrt(a) to 2^-45 at least: the hardware's (2^-23 at least) and one step of Newton's method, whose error is 3/2 of the square.  A
+// quotient and a root to the last bit, in every thread, are 2 us of 2048 x 8192.
+__device__ __forceinline__ double mx_rsqrt(double a)
+{
+    const double r = __builtin_amdgcn_rsq(a), next = r * __builtin_fma(-0.5 * a * r, r, 1.5);
+    return a > 0.0 && a < __builtin_inf() ? next : r;  // (0: infinite, infinite: 0, NaN)
 }
 
 // Piece i (eight values) of a row into its place.
@@ -151,8 +168,10 @@ __device__ __forceinline__ void mx_store8(const uint4 v, const uint4 g, double r
 }
 
 // One workgroup of W waves per row, NI pieces of eight values per thread, which stay in registers between the sum of squares and the codes.
+// Bound: HBM (2048 x 8192, e2m1: 23.6 us, 110 MB, 4.7 TB/s, the 8-bit form with a scale per row 22.4), for few rows the launch and a chain of
+// latencies (2.7 us on 1 x 4096).  A z in 32 bits, with 64 only for lanes near a border, is slower (28.7 us).
 template <int W, int NI, int TYPE>
-__global__ void __launch_bounds__(64 * W) add_rmsnorm_mx_kernel(int H8, double h, double eps, const uint4 *x, const uint4 *residual, const uint4 *__restrict__ gamma,
+__global__ void __launch_bounds__(64 * W) add_rmsnorm_mx_kernel(int H8, double inv_h, double eps, const uint4 *x, const uint4 *residual, const uint4 *__restrict__ gamma,
                                                                 void *__restrict__ codes, uint8_t *__restrict__ scales, uint4 *sum)
 {
     __shared__ double red[W];
@@ -175,7 +194,7 @@ __global__ void __launch_bounds__(64 * W) add_rmsnorm_mx_kernel(int H8, double h
         sqp_widen8(v[j], f);
         ss += mx_squares8(f);
     }
-    const double r = 1.0 / sqrt(mx_sum<W>(ss, red) / h + eps);
+    const double r = mx_rsqrt(__builtin_fma(mx_sum<W>(ss, red), inv_h, eps));
 #pragma unroll
     for (int j = 0; j < NI; j++) {
         const int i = threadIdx.x + 64 * W * j;
@@ -185,7 +204,7 @@ __global__ void __launch_bounds__(64 * W) add_rmsnorm_mx_kernel(int H8, double h
 
 // Rows too long for registers: the sums are read back from where this thread has written them.
 template <int TYPE>
-__global__ void __launch_bounds__(1024) add_rmsnorm_mx_long_kernel(int H8, double h, double eps, const uint4 *x, const uint4 *residual, const uint4 *__restrict__ gamma,
+__global__ void __launch_bounds__(1024) add_rmsnorm_mx_long_kernel(int H8, double inv_h, double eps, const uint4 *x, const uint4 *residual, const uint4 *__restrict__ gamma,
                                                                    void *__restrict__ codes, uint8_t *__restrict__ scales, uint4 *sum)
 {
     __shared__ double red[16];
@@ -198,7 +217,7 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_mx_long_kernel(int H8, doubl
         sqp_widen8(v, f);
         ss += mx_squares8(f);
     }
-    const double r = 1.0 / sqrt(mx_sum<16>(ss, red) / h + eps);
+    const double r = mx_rsqrt(__builtin_fma(mx_sum<16>(ss, red), inv_h, eps));
     for (int i = threadIdx.x; i < H8; i += 1024) mx_store8<TYPE>(sum[row + i], gamma[i], r, row + i, codes, scales);
 }
 
@@ -209,13 +228,13 @@ int launch_norm(int M, int H, const void *x, const void *residual, const void *g
     const uint4 *xp = (const uint4 *)x, *rp = (const uint4 *)residual, *gp = (const uint4 *)gamma;
     uint4 *sp = (uint4 *)sum;
     const dim3 grid((unsigned)M);
-#define ADD_RMSNORM_MX(W, NI) add_rmsnorm_mx_kernel<W, NI, TYPE><<<grid, 64 * W, 0, st>>>(H8, (double)H, (double)eps, xp, rp, gp, codes, scales, sp)
+#define ADD_RMSNORM_MX(W, NI) add_rmsnorm_mx_kernel<W, NI, TYPE><<<grid, 64 * W, 0, st>>>(H8, 1.0 / H, (double)eps, xp, rp, gp, codes, scales, sp)
     if (H8 <= 256) ADD_RMSNORM_MX(4, 1);
     else if (H8 <= 512) ADD_RMSNORM_MX(8, 1);
     else if (H8 <= 1024) ADD_RMSNORM_MX(16, 1);
     else if (H8 <= 2048) ADD_RMSNORM_MX(16, 2);
     else if (H8 <= 4096) ADD_RMSNORM_MX(16, 4);
-    else add_rmsnorm_mx_long_kernel<TYPE><<<grid, 1024, 0, st>>>(H8, (double)H, (double)eps, xp, rp, gp, codes, scales, sp);
+    else add_rmsnorm_mx_long_kernel<TYPE><<<grid, 1024, 0, st>>>(H8, 1.0 / H, (double)eps, xp, rp, gp, codes, scales, sp);
 #undef ADD_RMSNORM_MX
     return sqp_launch_status();
 }
@@ -260,7 +279,7 @@ extern "C" int sqp_mx_quantize_weight(int N, int K, const void *w, void *codes, 
     const int rc = check_blocks(N, K, SQP_E2M1, w, codes, scales);
     if (rc) return rc;
     if (N % 8) return SQP_ERR_SHAPE;
-    const dim3 grid((unsigned)((N + 63) / 64), (unsigned)((K + 255) / 256));
+    const dim3 grid((unsigned)((N + 127) / 128), (unsigned)((K + 255) / 256));
     if (grid.y > 65535u) return SQP_ERR_SHAPE;
     mx_quantize_weight_kernel<<<grid, 256, 0, (hipStream_t)stream>>>(N, K, (const h16 *)w, (uint4 *)codes, scales);
     return sqp_launch_status();

@@ -490,7 +490,9 @@ def test_attention_from_written_cache(sqp):
     a = sqp.paged_attention(q, c[0], c[1], order[None].cuda(), lens, starts, c[2], c[3], max_q=T, max_len=T)
     b = sqp.paged_attention(q, *half, order[None].cuda(), lens, starts, max_q=T, max_len=T)
     assert torch.equal(a, b)
-    # one token: the last
+    # one token, the last.  Over blocks p is rounded to fp16 once (2^-11 of sum p |v|), over fp16 taken in two parts (2^-22 of it); both
+    # outputs are rounded (half a step each), and the sum p |v| itself is an output over the values' magnitudes (half a step more).
     a1 = sqp.paged_attention(q[-1:], c[0], c[1], order[None].cuda(), lens, None, c[2], c[3], max_len=T)
     b1 = sqp.paged_attention(q[-1:], *half, order[None].cuda(), lens, max_len=T)
-    assert bool(((a1.double() - b1.double()).abs() <= 2.0 ** -10 * b1.double().abs() + 2.0 ** -20).all())
+    size = sqp.paged_attention(q[-1:], half[0], half[1].abs(), order[None].cuda(), lens, max_len=T).double()
+    assert bool(((a1.double() - b1.double()).abs() <= 2.0 ** -10 * b1.double().abs() + 1.01 * 2.0 ** -11 * size + 2.0 ** -24).all())
