@@ -110,10 +110,13 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
         if (is_x(i)) off[i] = (uint32_t)min(m0 + (64 * c + lane) / XLINE, a.M - 1) * x_row + 16u * (uint32_t)xpiece;
         else off[i] = (uint32_t)min(n0 + (64 * (c - T::XCOPIES) + lane) / WLINE, a.N - 1) * w_row + 16u * (uint32_t)wpiece;
     }
-    // A stage's copies; pieces past the end of K are taken from beyond the buffer (no tensor has 2^31 bytes).
-    uint32_t xpast = 0, wpast = 0;
+    // A stage's copies; pieces past the end of K are taken from beyond the buffer (no tensor has 2^31 bytes; the scalar offset stays within
+    // the row, so that they are beyond it whether or not the hardware's check counts that offset).
+    uint32_t xpast = 0, wpast = 0, at_stage = 0;
+    const uint32_t last_stage = (uint32_t)(blocks - 1) / BLOCKS;
     auto aim = [&](int stage) {
         const int left = blocks - BLOCKS * stage;
+        at_stage = min((uint32_t)stage, last_stage);
         xpast = xpiece < (FOUR ? left : 2 * left) ? 0u : 0x80000000u;
         wpast = FOUR ? xpast : wpiece < left ? 0u : 0x80000000u;
     };
@@ -121,9 +124,9 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
     // Weights of calls of few rows are read by one workgroup each (64 x 44032 x 8192: 55.0 us, 52.6 with the hint); where a stage takes half of
     // a line, the other half would be fetched again (16 rows of e4m3: 52.1, 59.5 with the hint).
     constexpr bool STREAM = BM <= 64 && WB == 128;
-    auto copy = [&](int stage, uint32_t slot, int i) {
+    auto copy = [&](uint32_t slot, int i) {
         const bool x = is_x(i);
-        const uint32_t offset = (uint32_t)stage * (x ? XB : WB), past = x ? xpast : wpast;
+        const uint32_t offset = at_stage * (x ? XB : WB), past = x ? xpast : wpast;
         if constexpr (T::COPIES % W == 0 && T::XCOPIES % W == 0) {
             if (STREAM && !x) copy_piece<true>(wbuf, off[i], past, offset, wave_base + slot, 1024u * (uint32_t)(W * i));
             else copy_piece<false>(x ? xbuf : wbuf, off[i], past, offset, wave_base + slot, 1024u * (uint32_t)(W * i));
@@ -219,7 +222,7 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
     for (int t = 0; t < SLOTS - 1; t++) {
         aim(first * SPC + t);
 #pragma unroll
-        for (int i = 0; i < T::PER; i++) copy(first * SPC + t, t * T::STAGE, i);
+        for (int i = 0; i < T::PER; i++) copy(t * T::STAGE, i);
         if constexpr (!DIRECT)
             if (t == 0) {
                 load_first_scales();
@@ -235,7 +238,7 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
     constexpr int EARLY = LEFT * T::PER / (LEFT + RT * CT);            // copies issued behind the meeting
     aim(first * SPC + SLOTS - 1);
 #pragma unroll
-    for (int i = 0; i < EARLY; i++) copy(first * SPC + SLOTS - 1, (SLOTS - 1) * T::STAGE, i);
+    for (int i = 0; i < EARLY; i++) copy((SLOTS - 1) * T::STAGE, i);
 
     // The order of instructions is fixed, and there are no branches (across one the compiler moves matrix instructions).  While a step's matrix
     // instructions run the next step's operands are fetched, and in a stage's first steps the copies of a stage to come are issued one by
@@ -299,7 +302,7 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
                         const int p = LAST ? at : LEFT + q;
                         if (p >= 0) {
 #pragma unroll
-                            for (int n = p * T::PER / OVER; n < (p + 1) * T::PER / OVER; n++) copy(c * SPC + u + SLOTS - (LAST ? 0 : 1), LAST ? slot : free, n);
+                            for (int n = p * T::PER / OVER; n < (p + 1) * T::PER / OVER; n++) copy(LAST ? slot : free, n);
                         }
                     }
                     __builtin_amdgcn_sched_barrier(0);
