@@ -512,6 +512,19 @@ def _shaped(t, shape, name):
         raise SqpError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
 
 
+def _placed(t, dtype, name):
+    """_dev for the operators on microscaled numbers, which refuse tensors of another device than the current one: kernels run there."""
+    p = _dev(t, dtype, name)
+    _on_current(**{name: t})
+    return p
+
+
+def _on_current(**tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise SqpError("%s must be on the current device (%d), not on %s" % (name, torch.cuda.current_device(), t.device))
+
+
 def _heads(t, name):
     """Pointer of a tensor [T, heads, D] fp16 whose tokens may lie apart (a view of a merged projection)."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
@@ -537,11 +550,12 @@ def _cache(k_cache, v_cache, k_scales, v_scales):
     kind, D = _CACHE_TYPES[k_cache.dtype], k_cache.shape[3]
     if kind == 4:
         D = 2 * D
+        _on_current(k_cache=k_cache, v_cache=v_cache)
         for at, (s, name) in enumerate(((k_scales, "k_scales"), (v_scales, "v_scales"))):
             if s is None:
                 raise SqpError("a cache of e2m1 blocks needs %s" % name)
             _shaped(s, tuple(k_cache.shape[:3]) + (D // 32,), name)
-            ptrs[2 + at] = _dev(s, torch.uint8, name)
+            ptrs[2 + at] = _placed(s, torch.uint8, name)
     elif kind:
         for at, (s, name) in enumerate(((k_scales, "k_scales"), (v_scales, "v_scales"))):
             if s is None:
@@ -585,6 +599,8 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, k_scales=None, v_scales=None, 
         _shaped(cos_sin, (n_positions, D), "cos_sin")
         _shaped(positions, (T,), "positions")
         cs, ps = _dev(cos_sin, torch.float32, "cos_sin"), _dev(positions, torch.int32, "positions")
+    if kind == 4:
+        _on_current(k=k, v=v, slots=slots, q=q, cos_sin=cos_sin, positions=positions, out=out)
     if T > 0:
         _check(lib().sqp_kv_cache_write(T, heads, kv_heads, D, kind, page, pages, qp, q_step, kp, _step(k), vp, _step(v), _dev(slots, torch.int32, "slots"),
                                         cs, ps, n_positions, *cache, op, _stream()), "sqp_kv_cache_write")
@@ -606,6 +622,8 @@ def kv_cache_read(slots, k_cache, v_cache, k_scales=None, v_scales=None, out=Non
     _shaped(k, (T, kv_heads, D), "k")
     _shaped(v, (T, kv_heads, D), "v")
     sp = _dev(slots, torch.int32, "slots")
+    if kind == 4:
+        _on_current(slots=slots, k=k, v=v)
     if T > 0:
         _check(lib().sqp_kv_cache_read(T, kv_heads, D, kind, page, pages, sp, *cache, _dev(k, torch.float16, "k"), _dev(v, torch.float16, "v"),
                                        _stream()), "sqp_kv_cache_read")
@@ -646,6 +664,8 @@ def paged_attention(q, k_cache, v_cache, page_table, seq_lens, q_starts=None, k_
     o = out if out is not None else torch.empty((T, heads, D), dtype=torch.float16, device=q.device)
     _shaped(o, (T, heads, D), "out")
     op = _dev(o, torch.float16, "out")
+    if kind == 4:
+        _on_current(q=q, page_table=page_table, seq_lens=seq_lens, q_starts=q_starts, out=o)
     max_q, max_len = int(max_q or 0) if q_starts is not None else 1, int(max_len or 0)
     scratch, nbytes = None, 0
     if T > 0 and not (out is not None and torch.cuda.is_current_stream_capturing()):
@@ -711,7 +731,7 @@ def mx_quantize(x, dtype=torch.uint8, out=None):
     kind = _mx_kind(dtype)
     R, K = x.shape
     codes, scales = _mx_out(out, R, K, kind, dtype, x.device)
-    _check(lib().sqp_mx_quantize(R, K, kind, _dev(x, torch.float16, "x"), _dev(codes, dtype, "codes"), _dev(scales, torch.uint8, "scales"), _stream()),
+    _check(lib().sqp_mx_quantize(R, K, kind, _placed(x, torch.float16, "x"), _placed(codes, dtype, "codes"), _placed(scales, torch.uint8, "scales"), _stream()),
            "sqp_mx_quantize")
     return codes, scales
 
@@ -725,7 +745,7 @@ def mx_quantize_weight(w, out=None):
             return o if type(o) is not int else _ended(o, "sqp_mx_quantize_weight")
     K, N = w.shape
     codes, scales = _mx_out(out, N, K, 4, torch.uint8, w.device)
-    _check(lib().sqp_mx_quantize_weight(N, K, _dev(w, torch.float16, "w"), _dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), _stream()),
+    _check(lib().sqp_mx_quantize_weight(N, K, _placed(w, torch.float16, "w"), _placed(codes, torch.uint8, "codes"), _placed(scales, torch.uint8, "scales"), _stream()),
            "sqp_mx_quantize_weight")
     return codes, scales
 
@@ -740,7 +760,7 @@ def mx_dequantize(codes, scales, out=None):
     R, K, kind = _mx_rows(codes, scales, "codes")
     x = out if out is not None else torch.empty((R, K), dtype=torch.float16, device=codes.device)
     _shaped(x, (R, K), "out")
-    _check(lib().sqp_mx_dequantize(R, K, kind, _dev(codes, codes.dtype, "codes"), _dev(scales, torch.uint8, "scales"), _dev(x, torch.float16, "out"), _stream()),
+    _check(lib().sqp_mx_dequantize(R, K, kind, _placed(codes, codes.dtype, "codes"), _placed(scales, torch.uint8, "scales"), _placed(x, torch.float16, "out"), _stream()),
            "sqp_mx_dequantize")
     return x
 
@@ -755,8 +775,8 @@ def _mx_gemm(silu, x, x_scales, w, w_scales, out):
         raise SqpError("x and w disagree on K")
     y = out if out is not None else torch.empty((M, N // 2 if silu else N), dtype=torch.float16, device=x.device)
     _shaped(y, (M, N // 2 if silu else N), "out")
-    args = [M, N, K, kind, silu, _dev(x, x.dtype, "x"), _dev(x_scales, torch.uint8, "x_scales"), _dev(w, torch.uint8, "w"), _dev(w_scales, torch.uint8, "w_scales"),
-            _dev(y, torch.float16, "out")]
+    args = [M, N, K, kind, silu, _placed(x, x.dtype, "x"), _placed(x_scales, torch.uint8, "x_scales"), _placed(w, torch.uint8, "w"), _placed(w_scales, torch.uint8, "w_scales"),
+            _placed(y, torch.float16, "out")]
     scratch, nbytes = None, 0
     if not (out is not None and torch.cuda.is_current_stream_capturing()):
         nbytes = int(lib().sqp_mx_gemm_scratch_bytes(M, N, K, kind))
@@ -805,7 +825,7 @@ def add_rmsnorm_mx(x, residual, gamma, eps, dtype=torch.uint8, out=None, sum_out
     codes, scales = _mx_out(out, M, H, kind, dtype, x.device)
     r = sum_out if sum_out is not None else torch.empty_like(x)
     _shaped(r, (M, H), "sum_out")
-    _check(lib().sqp_add_rmsnorm_mx(M, H, kind, _dev(x, torch.float16, "x"), _dev(residual, torch.float16, "residual"), _dev(gamma, torch.float16, "gamma"),
-                                    float(eps), _dev(codes, dtype, "codes"), _dev(scales, torch.uint8, "scales"), _dev(r, torch.float16, "sum_out"), _stream()),
+    _check(lib().sqp_add_rmsnorm_mx(M, H, kind, _placed(x, torch.float16, "x"), _placed(residual, torch.float16, "residual"), _placed(gamma, torch.float16, "gamma"),
+                                    float(eps), _placed(codes, dtype, "codes"), _placed(scales, torch.uint8, "scales"), _placed(r, torch.float16, "sum_out"), _stream()),
            "sqp_add_rmsnorm_mx")
     return codes, scales, r

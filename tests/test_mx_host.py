@@ -127,3 +127,16 @@ def test_binding_refusals():
                        (lambda: sqp.paged_attention(t, kc, kc, i[None], i[:1]), "GPU tensor")):
         with pytest.raises(sqp.SqpError, match=what):
             call()
+
+
+def test_tensors_of_another_device(monkeypatch):
+    """Every tensor of a call has to be on the current device: the one that is not is named."""
+    import types
+
+    import paper_2312_03788_amd as sqp
+    from paper_2312_03788_amd import binding
+    monkeypatch.setattr(binding.torch.cuda, "current_device", lambda: 1)
+    on = lambda i: types.SimpleNamespace(device=torch.device("cuda", i))
+    binding._on_current(x=on(1), out=None, w=on(1))
+    with pytest.raises(sqp.SqpError, match="w must be on the current device \\(1\\), not on cuda:0"):
+        binding._on_current(x=on(1), out=None, w=on(0))
