@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t xcd_run(uint32_t w, uint32_t total)
     return xcd * len + (xcd < more ? xcd : more) + w / XCDS;
 }
 
-template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, bool DIRECT>
+template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, int SC>
 struct Tile {
     static constexpr bool FOUR = XT == SQP_E2M1;
     static constexpr int BM = 32 * RT * WM, BN = 32 * CT * WN, W = WM * WN, THREADS = 64 * W;
@@ -59,19 +59,21 @@ struct Tile {
     static constexpr int XB = (FOUR ? 16 : 32) * BLOCKS, WB = 16 * BLOCKS;  // bytes of a row per stage
     static constexpr int XCOPIES = BM * XB / 1024, COPIES = XCOPIES + BN * WB / 1024;  // of 1 KB per stage
     static constexpr int PER = (COPIES + W - 1) / W;                    // per wave
-    static constexpr int SBM = (BM + 63) / 64 * 64;                     // rows of activations' scales (copies are of 64 rows)
-    static constexpr int STAGE = COPIES * 1024, SCALES = (SBM + BN) * 16;
-    static constexpr int SCOPIES = (SBM + BN) / 64, SPER = (SCOPIES + W - 1) / W;       // of 64 rows' scales of a chunk (DIRECT)
+    static constexpr int SBM = (BM + 63) / 64 * 64;                     // rows of activations' scales (copies are of 64 rows or 32)
+    static constexpr int HALVES = SC == 32 ? 2 : 1, SROW = 16 * HALVES; // chunks of 512 k, and bytes of a row, that scales are loaded for at once
+    static constexpr int STAGE = COPIES * 1024, SCALES = (SBM + BN) * SROW;
+    static constexpr int SCOPIES = SCALES / 1024, SPER = (SCOPIES + W * HALVES - 1) / (W * HALVES);  // of scales, per wave and 512 k (SC != 0)
+    static constexpr int YOUNGER = (SPC - 1) * PER;                     // copies of codes, at least, that are issued between scales and the meeting before their use
     static constexpr int LDS = SLOTS * STAGE + 2 * SCALES;
     static_assert(LDS <= 160 * 1024 && (XB < 256 || (COPIES % 4 == 0 && XCOPIES % 4 == 0 && W % 4 == 0)), "shared memory; the same piece in all of a wave's copies");
 };
 
-template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, bool DIRECT>
+template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, int SC>
 __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(WM * WN == 8 || RT * CT < 8 ? 2 : 1)))
 mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int chunks_per_part)
 {
-    typedef Tile<XT, RT, CT, WM, WN, BLK, SLOTS, DIRECT> T;
-    constexpr bool FOUR = T::FOUR;
+    typedef Tile<XT, RT, CT, WM, WN, BLK, SLOTS, SC> T;
+    constexpr bool FOUR = T::FOUR, DIRECT = SC != 0;
     constexpr int XFMT = FOUR ? 4 : 0, BM = T::BM, BN = T::BN, XB = T::XB, WB = T::WB, STEPS = T::STEPS, BLOCKS = T::BLOCKS, SPC = T::SPC;
     constexpr int AHEAD = (SLOTS - 2) * T::PER;     // copies that may be under way when the waves meet
     constexpr int W = T::W, SROWS = (BM + BN + T::THREADS - 1) / T::THREADS;  // waves; rows of scales per thread
@@ -139,17 +141,26 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
     uint8_t *const s_s = lds + SLOTS * T::STAGE;
     // DIRECT: copied as the codes are, since rows of them begin at words.
     const rsrc_t xsbuf = buffer_of(a.xs, (uint32_t)a.M * (uint32_t)blocks), wsbuf = buffer_of(a.ws, (uint32_t)a.N * (uint32_t)blocks);
-    uint32_t soff[DIRECT ? T::SPER : 1];
-    auto is_xs = [&](int i) { return (wave + W * i) % T::SCOPIES < T::SBM / 64; };
-    auto copy_scales = [&](int chunk, int i) {
-        copy_piece<false>(is_xs(i) ? xsbuf : wsbuf, soff[i], 0u, (uint32_t)min(16 * chunk, blocks - 16),
-                   __builtin_amdgcn_readfirstlane(base + SLOTS * T::STAGE + (chunk & 1) * T::SCALES + 1024u * (uint32_t)((wave + W * i) % T::SCOPIES)), 0u);
+    // SC = 32: those of two chunks at once, by two lanes a row, each kept inside the row by itself; one half of the copies is made in either
+    // of the two chunks before.  Rows 8 to 15 of 16 have their two in the other order, so that 16 rows lie in different banks.
+    uint32_t soff[DIRECT ? T::SPER : 1], smore[DIRECT ? T::SPER : 1];  // of the first half, and how much further those of the second are
+    auto scopy = [&](int i) { return (wave + W * i) % T::SCOPIES; };
+    const uint32_t second = T::HALVES == 2 && ((lane ^ lane >> 4) & 1) ? ~0u : 0u;
+    auto copy_scales = [&](int c, int i, uint32_t row) {  // of chunk c (and the one behind it)
+        const int start = 16 * c, at = min(start, blocks - 16), k = scopy(i);
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(base + SLOTS * T::STAGE + ((c - first) / T::HALVES & 1) * T::SCALES + 1024u * (uint32_t)k);
+        if constexpr (T::HALVES == 2) row += second & (uint32_t)(min(start + 16, blocks - 16) - at);
+        copy_piece<false>(k < T::SBM * T::SROW / 1024 ? xsbuf : wsbuf, row, 0u, (uint32_t)at, dst, 0u);
     };
     if constexpr (DIRECT) {
 #pragma unroll
         for (int i = 0; i < T::SPER; i++) {
-            const int row = 64 * ((wave + W * i) % T::SCOPIES) + lane;
-            soff[i] = (uint32_t)(is_xs(i) ? min(m0 + row, a.M - 1) : min(n0 + row - T::SBM, a.N - 1)) * (uint32_t)blocks;
+            auto offset = [&](int k) {
+                const int row = 64 / T::HALVES * scopy(k) + lane / T::HALVES;
+                return (uint32_t)(row < T::SBM ? min(m0 + row, a.M - 1) : min(n0 + row - T::SBM, a.N - 1)) * (uint32_t)blocks;
+            };
+            soff[i] = offset(i);
+            smore[i] = T::HALVES == 2 ? offset(i + T::SPER) - soff[i] : 0u;
         }
     }
     // Else through registers, a row or two per thread.
@@ -204,10 +215,14 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
         }
     };
     auto fetch_scale = [&](int chunk, int u, int n) {  // of stage u of the chunk
-        int at = u * BLOCKS + STEPS * h;
+        int at = u * BLOCKS + STEPS * h, buf = chunk & 1;
         // (a block past the end has zeros for codes, and some scale of its own row, so that no other row's NaN gets there)
-        if constexpr (DIRECT) at = min(at + max(16 * chunk - (blocks - 16), 0), 16 - STEPS);
-        const uint8_t *p = s_s + (chunk & 1) * T::SCALES + 16 * (n < CT ? T::SBM + wr + 32 * n : xr + 32 * (n - CT)) + at;
+        if constexpr (DIRECT) {
+            at = min(at + max(16 * chunk - (blocks - 16), 0), 16 - STEPS);
+            buf = (chunk - first) / T::HALVES & 1;
+            if constexpr (T::HALVES == 2) at += 16 * (((chunk - first) ^ l32 >> 3) & 1);
+        }
+        const uint8_t *p = s_s + buf * T::SCALES + T::SROW * (n < CT ? T::SBM + wr + 32 * n : xr + 32 * (n - CT)) + at;
         const uint32_t v = STEPS == 4 ? *(const uint32_t *)p : *(const uint16_t *)p;
         if (n < CT) next_wsc[n] = v;
         else next_xsc[n - CT] = v;
@@ -216,7 +231,10 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
     // the first stages, and the first chunk's scales
     if constexpr (DIRECT) {
 #pragma unroll
-        for (int i = 0; i < T::SPER; i++) copy_scales(first, i);
+        for (int i = 0; i < T::SPER; i++) {
+            copy_scales(first, i, soff[i]);
+            if constexpr (T::HALVES == 2) copy_scales(first, i + T::SPER, soff[i] + smore[i]);
+        }
     }
 #pragma unroll
     for (int t = 0; t < SLOTS - 1; t++) {
@@ -267,8 +285,8 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
                 constexpr bool LAST = s + 1 == STEPS;
                 constexpr int PF = (OPERANDS + (LAST ? LEFT : RT * CT) - 1) / (LAST ? LEFT : RT * CT);  // per matrix instruction: operands, scales
                 constexpr int PS = (RT + CT + LEFT - 1) / LEFT;
-                // (at a chunk's end its scales have to be there too: a stage's copies at least are younger than they)
-                constexpr int UNDER_WAY = DIRECT && SPC == 2 && u == SPC - 1 && AHEAD > T::PER ? T::PER : AHEAD;
+                // (at a chunk's end the next one's scales have to be there too)
+                constexpr int UNDER_WAY = DIRECT && u == SPC - 1 && AHEAD > T::YOUNGER ? T::YOUNGER : AHEAD;
                 if constexpr (!DIRECT && SLOTS == 2 && LAST && u == SPC - 1) store_scales(c + 1, by);
                 if constexpr (LAST) aim(c * SPC + u + SLOTS);
                 __builtin_amdgcn_sched_barrier(0);
@@ -294,7 +312,11 @@ mx_tiles_kernel(const SqpMxGemm a, int tiles_m, int tiles_n, int group_m, int ch
                     }
                     // the next chunk's scales
                     if constexpr (DIRECT && u == 0 && s == 0) {
-                        if (q < T::SPER) copy_scales(c + 1, q);
+#pragma unroll
+                        for (int n = q; n < T::SPER; n += RT * CT) {
+                            const int odd = T::HALVES == 2 ? (c - first) & 1 : 0;
+                            copy_scales(c - odd + T::HALVES, n + T::SPER * odd, soff[n] + (smore[n] & (uint32_t)-odd));
+                        }
                     }
                     // a stage's copies: behind the meeting before it, and in its first step
                     if constexpr (LAST || s == 0) {
@@ -375,18 +397,18 @@ __global__ void __launch_bounds__(256) mx_join_kernel(const SqpMxGemm a, int par
     sqp_mx_store4(a, (int)(i / n4), 4 * (int)(i % n4), s);
 }
 
-template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, bool DIRECT>
+template <int XT, int RT, int CT, int WM, int WN, int BLK, int SLOTS, int SC>
 int launch(const SqpMxTilePlan &p, const SqpMxGemm &a, hipStream_t st)
 {
-    typedef Tile<XT, RT, CT, WM, WN, BLK, SLOTS, DIRECT> T;
-    if (DIRECT && (a.K % 128 || a.K < 512)) return SQP_ERR_SHAPE;  // (the plan takes another tile)
+    typedef Tile<XT, RT, CT, WM, WN, BLK, SLOTS, SC> T;
+    if (SC != 0 && (a.K % 128 || a.K < 512)) return SQP_ERR_SHAPE;  // (the plan takes another tile)
     const int tm = (a.M + T::BM - 1) / T::BM, tn = (a.cols + T::BN - 1) / T::BN;
     const int chunks = (a.K + 511) / 512, per = (chunks + p.parts - 1) / p.parts, parts = (chunks + per - 1) / per;
     if ((long)tm * tn > 0x7fffffffL || parts > 65535) return SQP_ERR_SHAPE;
     SqpMxGemm b = a;
     if (parts == 1) b.part = nullptr;
     const dim3 grid((unsigned)(tm * tn), (unsigned)parts);
-    mx_tiles_kernel<XT, RT, CT, WM, WN, BLK, SLOTS, DIRECT><<<grid, T::THREADS, 0, st>>>(b, tm, tn, std::min(tm, 4), per);
+    mx_tiles_kernel<XT, RT, CT, WM, WN, BLK, SLOTS, SC><<<grid, T::THREADS, 0, st>>>(b, tm, tn, std::min(tm, 4), per);
     if (parts > 1) mx_join_kernel<<<(unsigned)(((long)a.M * (a.N / 4) + 255) / 256), 256, 0, st>>>(b, parts);
     return sqp_launch_status();
 }
@@ -395,20 +417,20 @@ template <int XT>
 int pick(const SqpMxTilePlan &p, const SqpMxGemm &a, hipStream_t st)
 {
     constexpr bool FOUR = XT == SQP_E2M1;
-    // (waves' tiles, waves; blocks per stage of e4m3 activations; slots for either type)
-#define TILE(i, RT, CT, WM, WN, BLK8, SLOTS4, SLOTS8, DIRECT)                                                                                    \
-    static_assert(SQP_MX_TILE[i].rows == 32 * RT * WM && SQP_MX_TILE[i].cols == 32 * CT * WN && SQP_MX_TILE[i].direct == DIRECT, "the tile's shape"); \
-    if (p.tile == i) return launch<XT, RT, CT, WM, WN, FOUR ? 8 : BLK8, FOUR ? SLOTS4 : SLOTS8, DIRECT>(p, a, st)
-    TILE(0, 4, 2, 2, 4, 4, 2, 3, true);
-    TILE(1, 2, 4, 2, 2, 4, 3, 4, true);
-    TILE(2, 2, 2, 2, 2, 4, 2, 3, true);
-    TILE(3, 2, 2, 2, 2, 4, 4, 5, true);
-    TILE(4, 2, 1, 1, 4, 8, 3, 4, true);
-    TILE(5, 1, 1, 1, 4, 8, 3, 3, true);
-    TILE(6, 1, 1, 1, 2, 4, 3, 3, true);
-    TILE(7, 2, 2, 2, 2, 4, 2, 3, false);
-    TILE(8, 2, 1, 1, 4, 4, 2, 2, false);
-    TILE(9, 1, 1, 1, 4, 4, 2, 2, false);
+    // (waves' tiles, waves; blocks per stage of e4m3 activations; slots, and scales of a row per copy, for either type)
+#define TILE(i, RT, CT, WM, WN, BLK8, SLOTS4, SC4, SLOTS8, SC8)                                                                                            \
+    static_assert(SQP_MX_TILE[i].rows == 32 * RT * WM && SQP_MX_TILE[i].cols == 32 * CT * WN && SQP_MX_TILE[i].direct == (SC4 != 0), "the tile's shape"); \
+    if (p.tile == i) return launch<XT, RT, CT, WM, WN, FOUR ? 8 : BLK8, FOUR ? SLOTS4 : SLOTS8, FOUR ? SC4 : SC8>(p, a, st)
+    TILE(0, 4, 2, 2, 4, 4, 2, 32, 3, 16);
+    TILE(1, 2, 4, 2, 2, 4, 3, 16, 4, 32);
+    TILE(2, 2, 2, 2, 2, 4, 2, 32, 3, 16);
+    TILE(3, 2, 2, 2, 2, 4, 4, 32, 5, 32);
+    TILE(4, 2, 1, 1, 4, 8, 3, 16, 4, 32);
+    TILE(5, 1, 1, 1, 4, 8, 3, 32, 3, 16);
+    TILE(6, 1, 1, 1, 2, 4, 3, 16, 3, 16);
+    TILE(7, 2, 2, 2, 2, 4, 2, 0, 3, 0);
+    TILE(8, 2, 1, 1, 4, 4, 2, 0, 2, 0);
+    TILE(9, 1, 1, 1, 4, 4, 2, 0, 2, 0);
 #undef TILE
     return SQP_ERR_SHAPE;
 }
