@@ -24,6 +24,8 @@
 // power limit leaves (1.8 of 2.4 GHz here).  A tile of 64 tokens takes a compute unit 2.2 to 2.35 us; without staging, maxima,
 // exponentials and barriers it still takes 1.8 to 2.0.  A 2048-token prompt of 32 heads: 59.4 us; its longest tile goes through
 // 32 steps of 64 tokens alone on its compute unit at 1.4 to 1.9 us each, in which latencies show that a second wave would hide.
+// Over e2m1 blocks (fp16 values by the time they are in shared memory, so that the products are those of an fp16 cache): 1024 tokens behind
+// 7168, 64 heads on 8, 282 us, 910 TFLOP/s.
 // Dropped (figures of the kernel as it was then): 64 rows per wave with one wave per SIMD (half the reads of shared memory, but nothing hides what the order of
 // instructions does not: 1288 us where 128-row tiles took 1240); stores spread over a step (their loads have less time: the
 // prompt 68.6 -> 74.6 us); K in shared memory with its scale multiplied in (a rounding more in the scores); p cut to 11 bits before

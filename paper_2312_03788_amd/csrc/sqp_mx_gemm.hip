@@ -19,9 +19,9 @@ struct Plan {
 // What a call takes in us, by the number of its workgroups: the least squares over 1799 timed calls (e2m1) and 1202 (e4m3) of every tile in one
 // to eight K parts, row counts from 1 to 4096 on eight layers from 1024 x 4096 to 44032 x 8192.  A round of workgroups, as many
 // as run at once, takes `tile` and for every 512 k `chunk[n - 1]` with n workgroups on a compute unit; a joining kernel takes `join`
-// and `join_mb` per MB of partial sums; the few-rows kernel `few` and per million weights `few_w` + rows * `few_mw`.  A call is off by 11 %
-// (root mean square); over the 207 sizes the tile and parts chosen by it take 2.4 % more than the best on average, 54 % at worst (1000 x 1024 x 4096,
-// e4m3: 20.9 us in four parts, 13.6 in one), 23 % beside that one.
+// and `join_mb` per MB of partial sums; the few-rows kernel `few` and per million weights `few_w` + rows * `few_mw`.  A call is off by 10 %
+// (root mean square); over the 207 sizes what is chosen by it takes 1 % more than the best on average, 52 % at worst (64 x 1024 x 4096,
+// e4m3: 11.7 us with the few-rows kernel, 7.7 in tiles), 25 % beside that one.
 struct Costs {
     float launch, join, join_mb, few, few_w, few_mw;
     struct {
@@ -29,20 +29,20 @@ struct Costs {
         int at_once;  // per compute unit
     } tile[SQP_MX_DIRECT_TILES];
 };
-constexpr Costs COSTS4 = {0.95f, 3.98f, 0.372f, 3.4f, 0.120f, 0.0045f,
-                          {{4.36f, {3.08f}, 1}, {3.16f, {2.28f}, 1}, {1.41f, {1.68f, 2.72f}, 2}, {1.82f, {1.33f}, 1}, {1.45f, {1.20f, 2.78f}, 2},
-                           {1.16f, {1.14f, 2.67f}, 2}, {1.17f, {0.77f, 1.30f, 2.20f, 3.24f}, 4}}};
-constexpr Costs COSTS8 = {0.49f, 3.97f, 0.358f, 3.4f, 0.130f, 0.0085f,
-                          {{6.51f, {4.06f}, 1}, {4.16f, {2.78f}, 1}, {2.24f, {1.81f, 3.54f}, 2}, {2.26f, {1.77f}, 1}, {2.53f, {1.38f}, 1},
-                           {1.69f, {1.20f, 2.82f}, 2}, {0.69f, {1.12f, 1.80f, 2.70f, 3.43f}, 4}}};
+constexpr Costs COSTS4 = {1.27f, 3.95f, 0.357f, 3.4f, 0.120f, 0.0045f,
+                          {{4.59f, {2.92f}, 1}, {2.94f, {2.28f}, 1}, {1.37f, {1.64f, 2.54f}, 2}, {1.98f, {1.25f}, 1}, {1.19f, {1.20f, 2.82f}, 2},
+                           {1.17f, {1.00f, 2.46f}, 2}, {1.12f, {0.75f, 1.27f, 2.17f, 3.22f}, 4}}};
+constexpr Costs COSTS8 = {0.67f, 4.09f, 0.331f, 3.4f, 0.130f, 0.0085f,
+                          {{6.65f, {4.08f}, 1}, {4.40f, {2.63f}, 1}, {2.18f, {1.78f, 3.54f}, 2}, {2.55f, {1.70f}, 1}, {2.54f, {1.31f}, 1},
+                           {1.59f, {1.19f, 2.82f}, 2}, {0.84f, {1.11f, 1.75f, 2.65f, 3.37f}, 4}}};
 constexpr int CUS = 256;
 
 int up(int a, int b) { return (a + b - 1) / b; }
 
-float tile_cost(const Costs &c, int t, int M, int N, int chunks, int parts)
+float tile_cost(const Costs &c, int t, int M, int N, int K, int parts)
 {
     const auto &k = c.tile[t];
-    const int per = up(chunks, parts), real = up(chunks, per);
+    const int chunks = up(K, 512), per = up(chunks, parts), real = up(chunks, per);
     const long groups = (long)up(M, SQP_MX_TILE[t].rows) * up(N, SQP_MX_TILE[t].cols) * real, room = CUS * k.at_once;
     const long full = groups / room, rest = groups % room;
     float us = full * (k.tile + per * k.chunk[k.at_once - 1]);
@@ -87,12 +87,12 @@ Plan plan(int M, int N, int K, int x_type, size_t room)
             const SqpMxTileShape &s = SQP_MX_TILE[t];
             const long groups = (long)up(M, s.rows) * up(N, s.cols), at_once = CUS * c.tile[t].at_once;
             for (int parts : {1, 2, 3, 4, 6, 8})
-                if (parts == 1 || (parts <= most && parts <= chunks && groups * parts <= at_once)) offer(t, parts, N, 0, tile_cost(c, t, M, N, chunks, parts));
+                if (parts == 1 || (parts <= most && parts <= chunks && groups * parts <= at_once)) offer(t, parts, N, 0, tile_cost(c, t, M, N, K, parts));
             // Whole rounds of this tile, and the columns left over in tiles of another shape.
             if (groups > at_once && groups % at_once) {
                 const int cols = (int)(groups / at_once * at_once / up(M, s.rows)) * s.cols;
                 for (int r = t + 1; r <= hi && cols > 0 && cols < N; r++)
-                    offer(t, 1, cols, r, tile_cost(c, t, M, cols, chunks, 1) + tile_cost(c, r, M, N - cols, chunks, 1) + 1.0f);
+                    offer(t, 1, cols, r, tile_cost(c, t, M, cols, K, 1) + tile_cost(c, r, M, N - cols, K, 1) + 1.0f);
             }
         }
     }

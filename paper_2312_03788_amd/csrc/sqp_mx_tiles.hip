@@ -9,7 +9,16 @@
 // The order of blocks within a stage is free as long as both operands and their scales have the same: lane half h takes blocks
 // STEPS h + s in step s, so that its scales lie together.  Of e4m3 activations a lane's first 16 values belong to the lower half's block and the
 // others to the upper half's (the instruction's order).
-// Scales come 16 (512 k) of a row at a time through registers, since rows of them begin at any byte.
+// Scales come 16 (512 k) of a row at a time, by direct loads too where rows of them begin at words, else through registers.  Every row's are a
+// line of their own: 4 % of the bytes, but a third of the lines asked for (256 x 256).  Where shared memory has room for it they come 32 at a
+// time: per 512 k the 256 x 256 tile (e2m1) takes 3.4 us instead of 3.5, 64 x 8192 x 8192 (e4m3) 24.9 us instead of 26.6, 32 x 8192 x 8192 (e2m1) 19.0
+// instead of 21.3.
+//
+// Measured: 2048 x 8192 x 8192 in whole rounds of 256 x 256, 62.5 us with e2m1 activations (4.4 PFLOP/s; a loop of the instruction alone
+// reaches 7.2), 94 with e4m3 (2.9; 4.3).  What is left out of a 512 k step of 3.45 us shows what it waits for: without the copies of codes 2.76,
+// without those of scales 3.17, all tiles from the same rows, so that every line is in the caches, 3.46: it is the copies' way through the
+// compute unit, not memory.  128 x 128 (e4m3), in the same order: 1.81, 1.31, 1.56, 1.86; a slot more 1.85, stages of twice the length 1.80,
+// operands fetched as early as can be the same.  Between idle gaps the same code is 15 % quicker: the power limit has its part.
 #include <algorithm>
 #include <type_traits>
 
@@ -417,6 +426,9 @@ template <int XT>
 int pick(const SqpMxTilePlan &p, const SqpMxGemm &a, hipStream_t st)
 {
     constexpr bool FOUR = XT == SQP_E2M1;
+    // 256 x 256 asks for the fewest bytes per product, but fills the compute units only in whole rounds of 256; the plan knows what each costs.  Of 128 x 128
+    // there are two: short slots with two workgroups per compute unit for many tiles (700 x 22016 x 4096, e4m3: 75.8 us, 82.1 deep), deep slots for
+    // up to one round (512 x 8192 x 8192, e2m1: 23.7 us, 28.2).
     // (waves' tiles, waves; blocks per stage of e4m3 activations; slots, and scales of a row per copy, for either type)
 #define TILE(i, RT, CT, WM, WN, BLK8, SLOTS4, SC4, SLOTS8, SC8)                                                                                            \
     static_assert(SQP_MX_TILE[i].rows == 32 * RT * WM && SQP_MX_TILE[i].cols == 32 * CT * WN && SQP_MX_TILE[i].direct == (SC4 != 0), "the tile's shape"); \
