@@ -20,8 +20,8 @@ struct Plan {
 // to eight K parts, row counts from 1 to 4096 on eight layers from 1024 x 4096 to 44032 x 8192.  A round of workgroups, as many
 // as run at once, takes `tile` and for every 512 k `chunk[n - 1]` with n workgroups on a compute unit; a joining kernel takes `join`
 // and `join_mb` per MB of partial sums; the few-rows kernel `few` and per million weights `few_w` + rows * `few_mw`.  A call is off by 10 %
-// (root mean square); over the 207 sizes what is chosen by it takes 1 % more than the best on average, 52 % at worst (64 x 1024 x 4096,
-// e4m3: 11.7 us with the few-rows kernel, 7.7 in tiles), 25 % beside that one.
+// (root mean square); over the 207 sizes what is chosen by it takes 1 % more than the best on average, 25 % at worst (1000 x 1024 x 4096,
+// e4m3: 17.7 us in six parts, 14.1 in one).
 struct Costs {
     float launch, join, join_mb, few, few_w, few_mw;
     struct {
@@ -70,7 +70,7 @@ Plan plan(int M, int N, int K, int x_type, size_t room)
     } else {
         const Costs &c = x_type == SQP_E2M1 ? COSTS4 : COSTS8;
         float best = 1e30f;
-        if (M <= 64) {
+        if (M <= (x_type == SQP_E2M1 ? 64 : 32)) {  // (e4m3, 33 to 64 rows: tiles are as quick on all sizes timed, 64 x 1024 x 4096 7.7 us instead of 11.8)
             best = c.few + 1e-6f * N * K * (c.few_w + c.few_mw * M);
             p.few = true;
         }
