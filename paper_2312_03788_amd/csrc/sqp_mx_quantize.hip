@@ -224,18 +224,24 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_mx_long_kernel(int H8, doubl
 template <int TYPE>
 int launch_norm(int M, int H, const void *x, const void *residual, const void *gamma, float eps, void *codes, uint8_t *scales, void *sum, hipStream_t st)
 {
+    constexpr int MOST = 1 << 21;  // rows of a launch, which has fewer than 2^32 threads
     const int H8 = H / 8;
-    const uint4 *xp = (const uint4 *)x, *rp = (const uint4 *)residual, *gp = (const uint4 *)gamma;
-    uint4 *sp = (uint4 *)sum;
-    const dim3 grid((unsigned)M);
-#define ADD_RMSNORM_MX(W, NI) add_rmsnorm_mx_kernel<W, NI, TYPE><<<grid, 64 * W, 0, st>>>(H8, 1.0 / H, (double)eps, xp, rp, gp, codes, scales, sp)
-    if (H8 <= 256) ADD_RMSNORM_MX(4, 1);
-    else if (H8 <= 512) ADD_RMSNORM_MX(8, 1);
-    else if (H8 <= 1024) ADD_RMSNORM_MX(16, 1);
-    else if (H8 <= 2048) ADD_RMSNORM_MX(16, 2);
-    else if (H8 <= 4096) ADD_RMSNORM_MX(16, 4);
-    else add_rmsnorm_mx_long_kernel<TYPE><<<grid, 1024, 0, st>>>(H8, 1.0 / H, (double)eps, xp, rp, gp, codes, scales, sp);
+    const uint4 *gp = (const uint4 *)gamma;
+    for (int first = 0; first < M; first += MOST) {
+        const size_t at = (size_t)first * H8;
+        const uint4 *xp = (const uint4 *)x + at, *rp = (const uint4 *)residual + at;
+        uint4 *sp = (uint4 *)sum + at;
+        uint8_t *cp = (uint8_t *)codes + at * (TYPE == SQP_E2M1 ? 4 : 8), *bp = scales + at / 4;
+        const dim3 grid((unsigned)min(M - first, MOST));
+#define ADD_RMSNORM_MX(W, NI) add_rmsnorm_mx_kernel<W, NI, TYPE><<<grid, 64 * W, 0, st>>>(H8, 1.0 / H, (double)eps, xp, rp, gp, cp, bp, sp)
+        if (H8 <= 256) ADD_RMSNORM_MX(4, 1);
+        else if (H8 <= 512) ADD_RMSNORM_MX(8, 1);
+        else if (H8 <= 1024) ADD_RMSNORM_MX(16, 1);
+        else if (H8 <= 2048) ADD_RMSNORM_MX(16, 2);
+        else if (H8 <= 4096) ADD_RMSNORM_MX(16, 4);
+        else add_rmsnorm_mx_long_kernel<TYPE><<<grid, 1024, 0, st>>>(H8, 1.0 / H, (double)eps, xp, rp, gp, cp, bp, sp);
 #undef ADD_RMSNORM_MX
+    }
     return sqp_launch_status();
 }
 

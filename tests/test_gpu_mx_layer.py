@@ -222,6 +222,26 @@ def test_largest_rows(sqp, kind):
     _same(codes.view(torch.uint8)[rows], scales[rows], y0, kind)
 
 
+@pytest.mark.parametrize("kind", ["e2m1", "e4m3"])
+def test_most_rows(sqp, kind):
+    """More short rows than one launch has threads for."""
+    M, H = (1 << 24) + 37, 32
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(13)
+    x, res = [torch.randn((M, H), generator=gen, device="cuda", dtype=torch.float16) for _ in range(2)]
+    gamma = torch.randn(H, generator=gen, device="cuda", dtype=torch.float16)
+    codes, scales, r = sqp.add_rmsnorm_mx(x, res, gamma, 1e-5, mx.DTYPES[kind])
+    rows = torch.tensor([0, 1, (1 << 21) - 1, 1 << 21, (1 << 23) + 5, (1 << 24) - 1, 1 << 24, M - 1], device="cuda")
+    y0, r0 = ref.add_rmsnorm(x[rows].cpu(), res[rows].cpu(), gamma.cpu(), 1e-5)
+    assert bool(((r[rows].cpu().double() - r0).abs() <= 2.0 ** -11 * r0.abs() + 2.0 ** -25).all())
+    _same(codes.view(torch.uint8)[rows], scales[rows], y0, kind)
+    codes, scales = sqp.mx_quantize(x, mx.DTYPES[kind])
+    _same(codes.view(torch.uint8)[rows], scales[rows], x[rows].cpu().double(), kind)
+    y = sqp.mx_gemm(codes, scales, *sqp.mx_quantize(x[:8]))
+    want, tol = mx.product(codes.view(torch.uint8)[rows].cpu(), scales[rows].cpu(), kind, *[t.cpu() for t in sqp.mx_quantize(x[:8])])
+    assert bool(((y[rows].cpu().double() - want).abs() <= tol).all())
+
+
 def test_largest_weight(sqp):
     K, N = 8192, 262000
     gen = torch.Generator(device="cuda")
