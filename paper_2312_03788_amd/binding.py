@@ -790,7 +790,9 @@ def _mx_gemm(silu, x, x_scales, w, w_scales, out):
 
 
 def mx_gemm(x, x_scales, w, w_scales, out=None):
-    """y [M, N] fp16 = x w^T on microscaled operands: x as mx_quantize gives it (either type), w as mx_quantize_weight does.
+    """y [M, N] fp16 = x w^T on microscaled operands: x as mx_quantize gives it (either type), w as mx_quantize_weight does.  fp32 sums of
+    products that are exact for e2m1 x; for e4m3 x a product smaller than 2^-7 of the largest of its eight neighbours along K (k // 8) is cut
+    by up to 2^-12 of that largest.
     Under graph capture a call with `out` allocates nothing, so that K is not split over workgroups."""
     if _fast is not None and isinstance(x, _Tensor) and x.is_cuda:
         dev = _current_device()
@@ -801,7 +803,7 @@ def mx_gemm(x, x_scales, w, w_scales, out=None):
 
 
 def mx_gemm_silu_mul(x, x_scales, w, w_scales, out=None):
-    """mx_gemm of a merged, interleaved gate/up weight with SiLU(gate) * up fused: y [M, N/2] fp16."""
+    """mx_gemm of a merged, interleaved gate/up weight with SiLU(gate) * up fused: y [M, N/2] fp16.  Sums and what e4m3 x loses: as there."""
     if _fast is not None and isinstance(x, _Tensor) and x.is_cuda:
         dev = _current_device()
         o = _fast.mx_gemm(1, x, x_scales, w, w_scales, out, dev, _raw_stream(dev))
