@@ -115,3 +115,30 @@ def test_product_e4m3_is_that_of_cut_products(sqp, plan, M, N, K):
         assert bool((err.abs() <= tol).all()), float((err.abs() / tol).max())
         # the whole: half a step of fp16 each, and independent additions
         assert float(err.norm()) <= 2.0 ** -11 * float(want.norm()) + sums ** 0.5 * 2.0 ** -24 * float(size.norm()) + 2.0 ** -25 * err.numel() ** 0.5
+
+
+@pytest.mark.parametrize("kind", ["e2m1", "e4m3"])
+@pytest.mark.parametrize("M,N,K", [(1, 8, 32), (5, 88, 1376), (33, 136, 96), (64, 1000, 2048), (70, 136, 4128), (140, 528, 4224), (300, 336, 1920), (257, 264, 512)])
+def test_product_of_whole_numbers(sqp, plan, M, N, K, kind):
+    """Operands whose products and sums fp32 holds exactly in any order (whole numbers up to 15, scales a power of two apart, so that no product is cut):
+    the automatic plan and every kernel give the sum rounded once, bit for bit and everywhere."""
+    g = ref.gen(M + N + K)
+    if kind == "e4m3":
+        n = torch.randint(-15, 16, (M, K), generator=g)
+        x = n.float().to(torch.float8_e4m3fn).view(torch.uint8)
+    else:
+        x = torch.randint(0, 256, (M, K // 2), generator=g).to(torch.uint8)
+    w = torch.randint(0, 256, (N, K // 2), generator=g).to(torch.uint8)
+    xs, ws = [torch.randint(126, 129, (R, K // 32), generator=g).to(torch.uint8) for R in (M, N)]
+    X, W = mx.values(x, xs, kind), mx.values(w, ws, "e2m1")
+    # multiples of 2^-1 2^-1 2^-1 (e4m3: whole x), sums below 2^24 of them
+    assert float((X.abs() @ W.abs().t()).max()) * (16 if kind == "e2m1" else 8) < 2 ** 24
+    want = (X @ W.t()).half()
+    dev = _gpu(x, xs, w, ws, kind)
+    for p in [(0, 0, 0, 0)] + FEW + TILES + TWO:
+        if not _fits(p, K):
+            continue
+        print("case whole numbers", M, N, K, kind, p, flush=True)
+        plan(*p)
+        y = sqp.mx_gemm(*dev).cpu()
+        assert torch.equal(y, want), (p, (y != want).nonzero()[:4].tolist())
