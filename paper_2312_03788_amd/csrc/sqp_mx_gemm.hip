@@ -131,6 +131,16 @@ extern "C" void sqp_debug_set_mx_plan(int kind, int a, int b, int c)
     g_hook_c = c;
 }
 
+extern "C" int sqp_debug_mx_plan(int M, int N, int K, int x_type, int *to)
+{
+    if (!to) return SQP_ERR_NULL;
+    if (!shape_ok(M, N, K) || (x_type != SQP_E2M1 && x_type != SQP_E4M3)) return SQP_ERR_SHAPE;
+    const Plan p = plan(M, N, K, x_type, (size_t)-1);
+    const int few[5] = {1, p.f.mt, p.f.nt, p.f.kw, 0}, tiles[5] = {2, p.t.tile, p.t.parts, p.cols, p.rest.tile};
+    std::copy_n(p.few ? few : tiles, 5, to);
+    return SQP_OK;
+}
+
 extern "C" size_t sqp_mx_gemm_scratch_bytes(int M, int N, int K, int x_type)
 {
     if (!shape_ok(M, N, K) || (x_type != SQP_E2M1 && x_type != SQP_E4M3)) return 0;
