@@ -85,7 +85,7 @@ int sqp_debug_read_probe(const void *src, size_t bytes, int nt, int blocks, void
 int sqp_debug_mfma_ceiling(const void *data, float *out, int blocks, int iters, void *stream);
 
 /* Plan of sqp_mx_gemm: kind 0 = automatic; 1 = the few-rows kernel with a 16-row tiles, b 16-column tiles and c waves (one of
- * the built combinations, else SQP_ERR_SHAPE); 2 = tile a in b K parts; 3 = tile a for the first c columns of tiles, tile b for the others. */
+ * the built combinations, else SQP_ERR_SHAPE); 2 = tile a (beyond the last: the last) in b K parts; 3 = tile a for the first c columns of tiles, tile b for the others. */
 void sqp_debug_set_mx_plan(int kind, int a, int b, int c);
 /* The plan of a call that is given all the scratch it asks for, plan [5]: {1, 16-row tiles, 16-column tiles, waves, 0} or {2, tile, K parts, columns in
  * that tile, tile of the columns behind them}.  SQP_ERR_SHAPE: no such product. */

@@ -5,8 +5,6 @@
 
 constexpr int SQP_MX_BLOCK = 32;
 
-template <> struct SqpCode<SQP_E2M1> { static constexpr float MAX = 6.0f; };
-
 #ifdef __HIPCC__
 // The scale's byte for a block whose largest magnitude has these bits: the least power of two with which that magnitude rounds to a
 // value of the type.  Of e2m1 (6 = 1.5 x 2^2 is the largest) magnitudes from 1.75 x 2^x on would round to 8 with the scale 2^(x - 2); of e4m3

@@ -28,9 +28,9 @@ struct SqpMxTileShape {
     bool direct;  // for K of whole 128, 512 at least
 };
 // The tiles' shapes; those of the same shape differ in how far ahead they load (sqp_mx_tiles.hip).
-constexpr int SQP_MX_TILES = 10, SQP_MX_DIRECT_TILES = 7;
+constexpr int SQP_MX_TILES = 8, SQP_MX_DIRECT_TILES = 7;
 constexpr SqpMxTileShape SQP_MX_TILE[SQP_MX_TILES] = {{256, 256, true}, {128, 256, true}, {128, 128, true}, {128, 128, true}, {64, 128, true}, {32, 128, true}, {32, 64, true},
-                                                          {128, 128, false}, {64, 128, false}, {32, 128, false}};
+                                                          {128, 128, false}};
 
 #ifdef __HIPCC__
 typedef int i32x4 __attribute__((ext_vector_type(4)));

@@ -64,7 +64,7 @@ Plan plan(int M, int N, int K, int x_type, size_t room)
     const int most = (int)std::min((size_t)8, std::max(room / one, (size_t)1));
     if (K % 128 || K < 512) {  // scales that do not begin at words, or no 16 of a row: no direct copies
         p.few = M <= 64;
-        p.t.tile = SQP_MX_DIRECT_TILES + (M > 64 ? 0 : M > 32 ? 1 : 2);
+        p.t.tile = SQP_MX_DIRECT_TILES;
         const long groups = (long)up(M, 128) * up(N, 128);
         if (!p.few) p.t.parts = (int)std::max(1L, std::min({2L * CUS / groups, (long)chunks / 2, (long)most}));
     } else {
@@ -104,7 +104,7 @@ Plan plan(int M, int N, int K, int x_type, size_t room)
         p.f = {g_hook_a, g_hook_b, g_hook_c};
     } else if (g_hook_kind == 2) {
         p.few = false;
-        p.t = {g_hook_a, std::min(std::max(1, g_hook_b), (int)std::min((size_t)64, std::max(room / one, (size_t)1)))};
+        p.t = {std::min(g_hook_a, SQP_MX_TILES - 1), std::min(std::max(1, g_hook_b), (int)std::min((size_t)64, std::max(room / one, (size_t)1)))};
         p.cols = N;
     } else if (g_hook_kind == 3) {
         p.few = false;

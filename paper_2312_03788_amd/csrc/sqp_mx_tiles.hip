@@ -441,8 +441,6 @@ int pick(const SqpMxTilePlan &p, const SqpMxGemm &a, hipStream_t st)
     TILE(5, 1, 1, 1, 4, 8, 3, 32, 3, 16);
     TILE(6, 1, 1, 1, 2, 4, 3, 16, 3, 16);
     TILE(7, 2, 2, 2, 2, 4, 2, 0, 3, 0);
-    TILE(8, 2, 1, 1, 4, 4, 2, 0, 2, 0);
-    TILE(9, 1, 1, 1, 4, 4, 2, 0, 2, 0);
 #undef TILE
     return SQP_ERR_SHAPE;
 }
