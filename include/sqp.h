@@ -296,7 +296,7 @@ int sqp_add_rmsnorm_mx(int M, int H, int type, const void *x, const void *residu
  * (cos_sin [n_positions][D] fp32: D/2 cosines, D/2 sines; NULL: no rotation; every product and sum rounded for itself), and keys and
  * values are quantised from these fp32 values.  q [T][heads][D], k, v [T][kv_heads][D] fp16 with the given distances between tokens (elements, multiples of 8),
  * q_out [T][heads][D] fp16 (heads == 0: no queries, q and q_out unused).  A token whose slot lies outside the cache (-1, say)
- * is not written; one whose position lies outside the table becomes NaN.  Two tokens in one slot: either may end there.
+ * is not written; one whose position lies outside the table becomes NaN.  Two tokens in one slot: a mixture of both may end there.
  * T == 0 enqueues nothing. */
 int sqp_kv_cache_write(int T, int heads, int kv_heads, int D, int type, int page, int pages, const void *q, long q_stride, const void *k,
                        long k_stride, const void *v, long v_stride, const int *slots, const float *cos_sin, const int *positions,
