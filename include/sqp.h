@@ -253,7 +253,7 @@ int sqp_mx_quantize(int R, int K, int type, const void *x, void *codes, uint8_t 
 int sqp_mx_dequantize(int R, int K, int type, const void *codes, const uint8_t *scales, void *x, void *stream);
 
 /* A weight w [K][N] fp16 (the orientation of Eq. 2, already smoothed) into e2m1 blocks along K: one row per output column, codes
- * [N][K/2], scales [N][K/32], which is what sqp_mx_quantize gives for w transposed.  K % 32 == 0, N % 8 == 0. */
+ * [N][K/2], scales [N][K/32], which is what sqp_mx_quantize gives for w transposed.  K % 32 == 0, K <= 16776960, N % 8 == 0. */
 int sqp_mx_quantize_weight(int N, int K, const void *w, void *codes, uint8_t *scales, void *stream);
 
 /* The linear layer on blocks: y[m][n] = fp16( sum_k x[m][k] w[n][k] ), the products of the codes multiplied by both blocks' scales on

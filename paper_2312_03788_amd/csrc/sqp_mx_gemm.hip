@@ -20,8 +20,9 @@ struct Plan {
 // to eight K parts, row counts from 1 to 4096 on eight layers from 1024 x 4096 to 44032 x 8192.  A round of workgroups, as many
 // as run at once, takes `tile` and for every 512 k `chunk[n - 1]` with n workgroups on a compute unit; a joining kernel takes `join`
 // and `join_mb` per MB of partial sums; the few-rows kernel `few` and per million weights `few_w` + rows * `few_mw`.  A call is off by 10 %
-// (root mean square); over the 207 sizes what is chosen by it takes 1 % more than the best on average, 25 % at worst (1000 x 1024 x 4096,
-// e4m3: 17.7 us in six parts, 14.1 in one).
+// (root mean square).  Over the 207 sizes what is chosen now takes 2 % more than the best of all forms on average, 28 % at worst (1000 x 1024 x 4096,
+// e4m3: 18.3 us in four parts, 14.3 in one); over 28 sizes of layers that the fit does not know (4096 x 11008, 11008 x 4096) 4 %, 28 % at worst
+// (333 x 11008 x 4096, e2m1: 24.6 us in tiles of 128 x 256, 19.3 in 128 x 128).
 struct Costs {
     float launch, join, join_mb, few, few_w, few_mw;
     struct {
@@ -63,6 +64,11 @@ Plan plan(int M, int N, int K, int x_type, size_t room)
     const size_t one = (size_t)M * N * sizeof(float);
     const int most = (int)std::min((size_t)8, std::max(room / one, (size_t)1));
     if (K % 128 || K < 512) {  // scales that do not begin at words, or no 16 of a row: no direct copies
+        // By the number of rows alone, which is not always the quicker: over 42 sizes 12 % more than the better of the two on average.  Up to 16 rows the
+        // few-rows kernel is, but for short K on many columns (1 x 4096 x 11040, e2m1: 10.7 us, tiles 14.5; 16 x 16384 x 480: 9.2, 6.3); up to
+        // 64 on up to 4096 columns mostly (64 x 2048 x 4128: 9.7, 11.1; but 64 x 4096 x 480: 9.3, 6.1), on more columns and long K tiles are (64 x 8192 x
+        // 1376: 16.8, 8.4; 64 x 4096 x 11040: 24.3, 17.5).  Parts: as many as fill two workgroups per compute unit (100 x 4096 x 11040: 19.1 us
+        // in eight, 55.6 whole), which a short K does not want (333 x 5120 x 4128: 24.9 in four, 18.3 whole).
         p.few = M <= 64;
         p.t.tile = SQP_MX_DIRECT_TILES;
         const long groups = (long)up(M, 128) * up(N, 128);
