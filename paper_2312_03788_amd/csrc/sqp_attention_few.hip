@@ -17,15 +17,16 @@
 // of p then, or 2^-35 of the row's largest where that is more).  The output's rounding is the only one left: the error of the 32
 // sequences' outputs below is 2.1e-4 of them instead of 2.6e-4, in the same time (149.2 us and 149.4); over codes it costs up to 3 % (16
 // sequences 39.0 us instead of 38.3, called again and again on the same cache), over e2m1 blocks, whose conversions keep the vector units busy half
-// of the time, 1 to 8 % (16 sequences 27.8 us instead of 25.8, one of 32000 tokens 35.7 instead of 35.3, 32 of up to 4096 tokens, 40 heads, 77.6
-// instead of 74.9).
+// of the time, 4 to 10 % (16 sequences 28.3 us instead of 25.8, one of 32000 tokens 36.3 instead of 34.8, 32 of up to 4096 tokens, 40 heads, 80
+// instead of 74).
 //
 // Measured, kernel alone: those 800 MB in 149 us (5.4 TB/s; a streaming read alone reaches 5.9 on this chip); one sequence of 32000
 // tokens, 40 heads, int8, 338 MB in 61 us (5.5 TB/s); 16 at up to 8192, 8 cached heads, e4m3, 166 MB in 36 us (4.6 TB/s, parts of unequal
 // length).  32 heads over 129 tokens: 6.1 us, the chain length, page, K, V.  The same over e2m1 blocks, calls in a row, joining included: the long
-// sequence's 174 MB in 36 us, the 16 sequences' 86 MB in 28: conversions, which take half of the vector units' time, and the ragged parts.
+// sequence's 174 MB in 36 us, the 16 sequences' 86 MB in 28: vector units busy half of the cycles, and the ragged parts.
 // Dropped (p was rounded once then, 26.1 us for the 16 sequences): 32 tokens per step and three workgroups per compute unit, 27.6 us; code for
-// four (128 registers) spills (67 us).
+// four (128 registers) spills (67 us).  And p's two parts converted in pairs: 1 % less, but other bits over codes, where the compiler takes the
+// second part from the exact product of p and the scale.
 #include "sqp_attention.h"
 
 namespace {
@@ -196,22 +197,12 @@ __global__ void __launch_bounds__(256, 2) attention_few_kernel(const SqpAttentio
             }
             h16x8 pf[NB / 2], pr[NB / 2];  // p to fp16's 11 bits, and to the next 11
 #pragma unroll
-            for (int i = 0; i < 4 * NB; i += 2) {
-                f32x2 pv;
-#pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    const float p = sqp_exp2(BLOCKS ? __builtin_fmaf(t[i + e], a.scale2, -m) : t[i + e] - m);
-                    l += p;
-                    pv[e] = !CODES ? p : p * vs[i >> 2][(i + e) & 3];
-                }
-                const h16x2 first = __builtin_convertvector(pv, h16x2);  // (two per instruction; the differences read the halves as they are)
-                const f32x2 left = {__builtin_fmaf((float)first.x, -1.f, pv.x), __builtin_fmaf((float)first.y, -1.f, pv.y)};
-                const h16x2 second = __builtin_convertvector(left, h16x2);
-#pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    pf[i >> 3][(i + e) & 7] = first[e];
-                    pr[i >> 3][(i + e) & 7] = second[e];
-                }
+            for (int i = 0; i < 4 * NB; i++) {
+                const float p = sqp_exp2(BLOCKS ? __builtin_fmaf(t[i], a.scale2, -m) : t[i] - m);
+                l += p;
+                const float pv = !CODES ? p : p * vs[i >> 2][i & 3];
+                pf[i >> 3][i & 7] = (h16)pv;
+                pr[i >> 3][i & 7] = (h16)(pv - (float)pf[i >> 3][i & 7]);
             }
 #pragma unroll
             for (int q = 0; q < NB / 2; q++) {

@@ -47,6 +47,7 @@ __device__ __forceinline__ uint32_t sqp_quad_max(uint32_t x)
 // Eight e2m1 codes of a word as values times the scale, fp32 (exact; a scale of NaN makes NaN of them).
 __device__ __forceinline__ void sqp_mx_e2m1_values8(uint32_t w, float scale, float *f)
 {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
     const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
     const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
     f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;

@@ -3,8 +3,6 @@
 #pragma once
 #include "sqp_common.h"
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
 // Codes of a type: element size, and the largest magnitude a code stands for.
 template <int TYPE> struct SqpCode;
 template <> struct SqpCode<SQP_FP16> { static constexpr int BYTES = 2; };
