@@ -3,7 +3,8 @@
 // 1 x 4096 x 4096: 4.0 us, a launch, one round of loads and the waves' join; 1 x 44032 x 8192: 43.4 us, 191 MB, 4.4 TB/s.  What bounds it is how
 // its loads follow each other, not the memory: a wave asks for a round of 512 k, waits, multiplies and asks for the next, and 5120 columns are
 // 320 workgroups on 256 compute units (1 x 5120 x 13824: 12.8 us).  The kernels for integer weights, which load ahead, read at up to 5.6 TB/s
-// (one row, these layers: 33 and 11.2 us).  From 16 rows on small tiles read large weights as fast and the activations once (16 x 44032 x 8192: 53.2 us here, 40.5 in tiles of 32 x 64).
+// (one row, these layers: 33 and 11.2 us).  From 16 rows on small tiles read large weights as fast and the activations once (16 x 44032 x
+// 8192: 53.2 us here, 40.5 in tiles of 32 x 64).
 //
 // A workgroup takes 16 NT columns and all rows (16 MT); its KW waves take 512 k in turn and add their sums through shared
 // memory at the end.  Per 512 k and 16 columns a wave has four 16x16x128 instructions: lane (c, g) holds the 32 codes of

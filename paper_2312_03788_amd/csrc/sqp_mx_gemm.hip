@@ -92,8 +92,8 @@ Plan plan(int M, int N, int K, int x_type, size_t room)
         for (int t = lo; t <= hi; t++) {
             const SqpMxTileShape &s = SQP_MX_TILE[t];
             const long groups = (long)up(M, s.rows) * up(N, s.cols), at_once = CUS * c.tile[t].at_once;
-            // K parts up to one and a half times what runs at once (which bounds their sums: 96 MiB in the largest tile): 16 x 44032 x 8192, e4m3, 45.5 us in 688 workgroups on 512 places, 51 in smaller tiles
-            // without parts.
+            // K parts up to one and a half times what runs at once (which bounds their sums: 96 MiB in the largest tile): 16 x 44032 x 8192, e4m3, 45.5 us
+            // in 688 workgroups on 512 places, 51 in smaller tiles without parts.
             for (int parts : {1, 2, 3, 4, 6, 8})
                 if (parts == 1 || (parts <= most && parts <= chunks && 2 * groups * parts <= 3 * at_once)) offer(t, parts, N, 0, tile_cost(c, t, M, N, K, parts));
             // Whole rounds of this tile, and the columns left over in tiles of another shape.  (Not for few rows, which wait for memory in either
