@@ -262,8 +262,8 @@ int sqp_mx_quantize_weight(int N, int K, const void *w, void *codes, uint8_t *sc
  * smaller than 2^-7 of the largest of its eight is off by up to 2^-12 of that largest, the others by nothing.  So the sum is off by up to
  * 7 * 2^-12 of the sum of the eights' largest products, besides fp32's own additions; beside a channel of outliers, or where large products cancel, that is
  * what is left of its seven neighbours.  (Uniformly random codes lose up to 2e-4 of sum |x w|, a sum's outputs 2.1e-4 rms with their rounding.)
- * x: M rows of x_type (SQP_E2M1 or SQP_E4M3) with their scales, w: N rows of e2m1 with theirs.  M, N, K > 0, N % 8 == 0, K % 32 == 0.  silu_mul != 0: the columns alternate (gate j, up j) (sqp_interleave_gate_up), N % 16 == 0, and
- * y [M][N/2] = fp16(SiLU(g) u) of the fp32 sums.  A block that is NaN makes NaN of its row (x) or column (w).  Deterministic.
+ * x: M rows of x_type (SQP_E2M1 or SQP_E4M3) with their scales, w: N rows of e2m1 with theirs.  M, N, K > 0, N % 8 == 0, K % 32 == 0.
+ * silu_mul != 0: the columns alternate (gate j, up j) (sqp_interleave_gate_up), N % 16 == 0, and y [M][N/2] = fp16(SiLU(g) u) of the fp32 sums.  A block that is NaN makes NaN of its row (x) or column (w).  Deterministic.
  * scratch: of this call alone until its work has run, sqp_mx_gemm_scratch_bytes() for the preferred plan (at most 96 MiB); smaller or NULL:
  * a plan that fits.  No other workspace: calls may overlap with anything. */
 size_t sqp_mx_gemm_scratch_bytes(int M, int N, int K, int x_type);
